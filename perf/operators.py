@@ -204,9 +204,9 @@ def _run_own(s):
             out.append(mix.router_topk_grad(s["logits"], idx, weights, s["d_weights"], act=s["act_id"], renormalise=s["renorm"]))
         return out
     if s["op"] == "balance":
-        loss, counts, mean_p = mix.router_balance(s["logits"], s["idx"], s["seg"], act=s["act_id"])
-        grad = mix.router_balance_grad(s["logits"], s["idx"], counts, s["d_loss"], s["seg"], act=s["act_id"])
-        return [loss, counts, mean_p, grad]
+        loss, counts, mean_p, rows = mix.router_balance(s["logits"], s["idx"], s["seg"], act=s["act_id"])
+        grad = mix.router_balance_grad(s["logits"], s["idx"], counts, rows, s["d_loss"], s["seg"], act=s["act_id"])
+        return [loss, counts, mean_p, rows, grad]
     if s["op"] == "linear":
         codes, scale = mix.quantize_rows_i8(s["x"])
         return mix.linear_i8(codes, scale, s["w"], s["w_scale"], bias=s["bias"], dtype=s["x"].dtype)
@@ -326,7 +326,7 @@ def _plain_balance(s):
     if s["act"] == "sigmoid":
         d = d / (1 + torch.exp(x))
     d = torch.where(on[:, None] & (x > -math.inf), d, 0.0)
-    return [loss.float(), counts.int(), mean_p.float(), d.to(s["logits"].dtype)]
+    return [loss.float(), counts.int(), mean_p.float(), rows.int(), d.to(s["logits"].dtype)]
 
 
 def _quantized(x):
@@ -442,7 +442,7 @@ def _exact_balance(s):
     x, E = s["logits"].double(), s["E"]
     idx, seg = s["idx"], s["seg"].tolist()
     p = _exact_p(x, s["act"])
-    losses, counts, means = [], [], []
+    losses, counts, means, ns = [], [], [], []
     d = torch.zeros_like(x)
     for i in range(s["requests"]):
         a, b = seg[i], seg[i + 1]
@@ -456,10 +456,12 @@ def _exact_balance(s):
         losses.append(E * (f * mean).sum())
         counts.append(c.int())
         means.append(mean)
+        ns.append(n)
         h = s["d_loss"][i].double() * E / max(n, 1) * f
         di = pi * (h[None] - (pi * h[None]).sum(1, keepdim=True))
         d[a:b] = di * torch.sigmoid(-x[a:b]) if s["act"] == "sigmoid" else di
-    return [torch.stack(losses), torch.stack(counts), torch.stack(means), torch.where(p > 0, d, 0.0)]
+    ns = torch.tensor(ns, dtype=torch.int32, device="cuda")
+    return [torch.stack(losses), torch.stack(counts), torch.stack(means), ns, torch.where(p > 0, d, 0.0)]
 
 
 def _exact_codes(x):
