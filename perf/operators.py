@@ -7,9 +7,9 @@ Four operators through the public entry points:
   balance  how evenly the router spreads each request's tokens: per-expert counts, mean probabilities and the balance
            loss, `router_balance`, and the loss's gradient, `router_balance_grad`
   linear   y = x W^T with x quantised to 8-bit integers per token and W held in 8-bit integers with a scale per output
-           channel: `quantize_rows_i8`, `linear_i8`
+           channel: `quantize_rows`, `linear_int`
   experts  the same product where each token goes through the experts that its router chose: `expert_order`,
-           `quantize_rows_i8` in the order of the experts, `linear_i8_grouped`, and, where a token's results are summed
+           `quantize_rows` in the order of the experts, `linear_int_grouped`, and, where a token's results are summed
            again, `expert_combine`
 """
 import math
@@ -208,11 +208,11 @@ def _run_own(s):
         grad = mix.router_balance_grad(s["logits"], s["idx"], counts, rows, s["d_loss"], s["seg"], act=s["act_id"])
         return [loss, counts, mean_p, rows, grad]
     if s["op"] == "linear":
-        codes, scale = mix.quantize_rows_i8(s["x"])
-        return mix.linear_i8(codes, scale, s["w"], s["w_scale"], bias=s["bias"], dtype=s["x"].dtype)
+        codes, scale = mix.quantize_rows(s["x"])
+        return mix.linear_int(codes, scale, s["w"], s["w_scale"], bias=s["bias"], dtype=s["x"].dtype)
     offsets, order, position = mix.expert_order(s["idx"], s["E"])
-    codes, scale = mix.quantize_rows_i8(s["x"], order=order, k=s["k"])
-    y = mix.linear_i8_grouped(codes, scale, s["w"], s["w_scale"], offsets, dtype=s["x"].dtype)
+    codes, scale = mix.quantize_rows(s["x"], order=order, k=s["k"])
+    y = mix.linear_int_grouped(codes, scale, s["w"], s["w_scale"], offsets, dtype=s["x"].dtype)
     return mix.expert_combine(y, s["weights"], position) if s["combine"] else y
 
 
