@@ -504,6 +504,113 @@ int mix_debug_phase_clocks(mix_ctx* ctx, unsigned long long* out32);
 int mix_sae_apply_static(void* hidden, int n_rows, int d_model, const mix_sae_weights* w, const mix_sae_app* app,
                          int* topk_idx, float* topk_val, void* stream, char* errbuf, int errbuf_len);
 
+/* ---------------------------------------------------------------------------------------
+ * Behind the router: selection, balance and the experts' products.
+ *
+ * mix_apply_router() steers router logits.  These calls are what follows it in an MoE layer, and what an
+ * application needs to see and to train such a steering: which experts the (steered) logits choose, how a request's tokens
+ * spread over the experts, the balance loss on that, and the products of the experts' 8-bit weights.
+ * (The paper names router steering only -- Table 1, row 7; the arithmetic here is the standard one.)
+ *
+ * They need no context.  All pointers are device pointers on the CURRENT device unless a line says otherwise; every call
+ * enqueues kernels on `stream` and returns, allocates nothing and synchronises nothing (mix_linear_int_status excepted), and may be
+ * captured.  Scratch memory, where a call needs any, is the caller's: it holds nothing between calls, and calls that may
+ * overlap need one each.  errbuf (host, may be NULL) receives a message for a call that fails.  Where a call
+ * fails nothing has been enqueued, unless the code is MIX_ERR_CUDA.
+ * Two calls with the same inputs give the same bits: nothing is added up in an order that depends on timing. */
+enum { MIX_DTYPE_F32 = 0, MIX_DTYPE_BF16 = 1, MIX_DTYPE_F16 = 2 };   /* element types of the tensors of these calls */
+#define MIX_ORDER_MAX_ENTRIES 16777216    /* mix_expert_order: most entries of a call */
+#define MIX_BALANCE_MAX_SEGMENTS 65536    /* mix_router_balance: most segments of a call */
+#define MIX_I8_MAX_K 131056               /* 8-bit products: longest row (a sum of 131071 products of -128 and -128 still fits in 31 bits) */
+
+/* The k experts of each token.  logits: dtype [T, n_experts], rows ld elements apart.  idx int32 [T, k]: the k largest logits of
+   the row, largest first, of equal ones the lower index first; weights fp32 [T, k]: with p = softmax of the row
+   (act = MIX_ACT_SOFTMAX) or p = sigmoid of each logit (MIX_ACT_SIGMOID), p[idx], or, with renormalise != 0,
+   p[idx] / sum of the chosen p.
+   Steered rows: an expert at -inf (or NaN) is never chosen and has no probability; where fewer than k are left, the last entries
+   are -1 with weight 0.  Experts at +inf are chosen first and share the softmax alone, in equal parts -- the limit of equal logits
+   that grow without bound.  n_live (device int32[1], NULL = T): rows at and behind it are padding, they are not read and get -1 and 0.
+   Errors: OUT_OF_RANGE (T < 0, n_experts outside [1, 512], k outside [1, min(16, n_experts)], ld < n_experts), INVALID_ARG. */
+int mix_router_topk(const void* logits, int dtype, long long ld, int T, int n_experts, int k, int act, int renormalise, const int* n_live,
+                    int* idx, float* weights, void* stream, char* errbuf, int errbuf_len);
+
+/* Gradient of the weights: d_logits (dtype [T, n_experts], rows ld_d apart, every entry written) of sum_j d_weights[t, j] weights[t, j],
+   for the idx and weights that mix_router_topk() gave for these logits, act and renormalise.  Entries with idx -1 do not count, whatever
+   stands in their d_weights.  d_logits may not overlap logits. */
+int mix_router_topk_grad(const void* logits, int dtype, long long ld, int T, int n_experts, int k, int act, int renormalise, const int* idx,
+                         const float* weights, const float* d_weights, void* d_logits, long long ld_d, void* stream, char* errbuf,
+                         int errbuf_len);
+
+/* The tokens by expert: a stable counting sort of the n = T * k entries of idx.  order int32 [n]: the entries (t * k + j) of expert 0, then
+   those of expert 1, and so on, each expert's in rising order; -1 behind them.  offsets int32 [n_experts + 1]: expert e's are
+   order[offsets[e] .. offsets[e + 1]), so differences of neighbours are the per-expert counts.  position int32 [n]: the place of an entry in
+   `order`, -1 for entries that name no expert (idx outside [0, n_experts)).
+   workspace: mix_expert_order_workspace(n, n_experts) bytes (0 for up to 4096 entries; negative: a mix_status).
+   Errors: OUT_OF_RANGE (n outside [0, MIX_ORDER_MAX_ENTRIES], n_experts), INVALID_ARG. */
+long long mix_expert_order_workspace(long long n, int n_experts);
+int mix_expert_order(const int* idx, long long n, int n_experts, int* offsets, int* order, int* position, void* workspace,
+                     long long workspace_bytes, void* stream, char* errbuf, int errbuf_len);
+
+/* How evenly the router spreads the tokens of each segment (a request, a sequence, a batch), and the balance loss on it.
+   seg int32 [n_seg + 1]: segment s is the rows seg[s] .. seg[s + 1) (offsets that do not fall, as mix_set_request_map's requests lie one
+   behind the other); NULL with n_seg = 1: all T rows.  idx int32 [T, k] as from mix_router_topk(): a row counts if it names an expert
+   (a row of -1, and a row outside every segment, does not).  With p the softmax of the row's logits, or its sigmoids divided by
+   their sum:
+     counts[s, e]  int32: entries of idx that name e        rows[s]  int32: rows that count
+     mean_p[s, e]  fp32: mean of p[., e] over those rows
+     loss[s]       fp32: n_experts * sum_e f_e mean_p[s, e],  f_e = counts[s, e] / sum_e counts[s, e];  0 without rows.
+                   1 where both are even, n_experts where all went to one.
+   Logits of +-inf and NaN count as in mix_router_topk().
+   workspace: mix_router_balance_workspace(T, n_experts, n_seg) bytes (negative: a mix_status).
+   Errors: as mix_router_topk(), OUT_OF_RANGE (n_seg outside [1, MIX_BALANCE_MAX_SEGMENTS]). */
+long long mix_router_balance_workspace(int T, int n_experts, int n_seg);
+int mix_router_balance(const void* logits, int dtype, long long ld, const int* idx, int T, int n_experts, int k, int act, const int* seg,
+                       int n_seg, float* loss, int* counts, float* mean_p, int* rows, void* workspace, long long workspace_bytes,
+                       void* stream, char* errbuf, int errbuf_len);
+
+/* Gradient of the balance loss: d_logits (every entry written; 0 in rows that do not count) of sum_s d_loss[s] loss[s], with the counts and
+   rows that the forward call gave.  No gradient passes through the counts.  d_logits may not overlap logits. */
+int mix_router_balance_grad(const void* logits, int dtype, long long ld, const int* idx, int T, int n_experts, int k, int act, const int* seg,
+                            int n_seg, const int* counts, const int* rows, const float* d_loss, void* d_logits, long long ld_d, void* stream,
+                            char* errbuf, int errbuf_len);
+
+/* Rows of x (bf16 or fp16, [x_rows, d], rows ld apart) as 8-bit integers with one scale each: scale[i] = max|x_i| / 127,
+   codes[i, :] = x_i * 127 / max|x_i| rounded to the nearest, halves to even, from -127 to 127; int8 [n_rows, d], densely packed.
+   A row of zeros gives zeros and scale 0; a row with an infinity or NaN gives zeros and scale NaN, so that its products are NaN.
+   order == NULL: row i is row i of x (n_rows = x_rows).  Otherwise row i is row order[i] / k of x -- mix_expert_order()'s order puts each
+   expert's tokens next to each other -- and an order[i] below 0 or naming no row gives zeros and scale 0.
+   Weights are quantised by the same call: a row of W is an output channel.
+   Errors: OUT_OF_RANGE (d outside [16, MIX_I8_MAX_K], ld < d, k < 1), UNSUPPORTED (d % 16), INVALID_ARG (codes not on 16 bytes). */
+int mix_quantize_rows(const void* x, int dtype, long long ld, int x_rows, const int* order, int k, int n_rows, int d, signed char* codes,
+                         float* scale, void* stream, char* errbuf, int errbuf_len);
+
+/* out[t, n] = (sum_i codes[t, i] W[n, i]) scale[t] w_scale[n] + bias[n].  codes int8 [T, K] and W int8 [N, K] densely packed,
+   scale fp32 [T], w_scale fp32 [N], bias fp32 [N] or NULL; out: out_dtype [T, N], rows ld_out apart.  The sum is exact, the rest fp32,
+   rounded once.
+   Errors: OUT_OF_RANGE (T < 0, N < 1, K outside [16, MIX_I8_MAX_K], ld_out < N), UNSUPPORTED (K % 16), INVALID_ARG (codes or W not on
+   16 bytes). */
+int mix_linear_int(const signed char* codes, const float* scale, int T, int K, const signed char* W, const float* w_scale, int N,
+                  const float* bias, void* out, int out_dtype, long long ld_out, void* stream, char* errbuf, int errbuf_len);
+
+/* The same with a weight set per group of rows: rows offsets[e] .. offsets[e + 1) of codes go through W[e] (int8 [n_experts, N, K], w_scale and
+   bias fp32 [n_experts, N]).  offsets int32 [n_experts + 1], on the device: how many rows an expert has is never read by the host.  Rows
+   of `out` in front of offsets[0] and from offsets[n_experts] on are left as they were. */
+int mix_linear_int_grouped(const signed char* codes, const float* scale, int n_rows, int K, const signed char* W, const float* w_scale,
+                          int n_experts, int N, const int* offsets, const float* bias, void* out, int out_dtype, long long ld_out,
+                          void* stream, char* errbuf, int errbuf_len);
+
+/* Copy the status word of the 8-bit products on the current device to *bits (host) and clear it: MIX_STATUS_WAIT_TIMEOUT after a bounded wait
+   inside a product kernel ran out, in which case the results since the last call are invalid.  Synchronises `stream`. */
+int mix_linear_int_status(unsigned* bits, void* stream, char* errbuf, int errbuf_len);
+
+/* The experts' results summed over each token's experts: out[t, :] = sum_j weights[t, j] y[position[t, j], :], j rising, in fp32, rounded
+   once.  y: dtype [y_rows, N], rows ld_y apart, in mix_expert_order()'s order; position int32 [T, k] from the same call, entries outside
+   [0, y_rows) do not count (nor what stands in their weights).  out: dtype [T, N], rows ld_out apart; a token without experts gets zeros.
+   out may not overlap y.
+   Errors: OUT_OF_RANGE (T < 0, N < 1, k outside [1, 16], ld below N), INVALID_ARG. */
+int mix_expert_combine(const void* y, int dtype, long long ld_y, int y_rows, const float* weights, const int* position, int T, int k, int N,
+                       void* out, long long ld_out, void* stream, char* errbuf, int errbuf_len);
+
 #ifdef __cplusplus
 }
 #endif

@@ -13,7 +13,7 @@ LIB_PATH = os.path.join(PKG_DIR, "libmix.so")
 FAST_PATH = os.path.join(PKG_DIR, "_fastcall.so")      # CPython module of the binding's per-step calls, linked to libmix.so
 
 SOURCES = ["mix_api.cu", "route_probe_steer.cu", "probe_tc.cu", "sae_front.cu", "sae_simt_edit_only.cu", "sae_encode_tc.cu", "sae_tail.cu",
-           "sae_static.cu"]
+           "sae_static.cu", "router_select.cu", "router_balance.cu", "linear_int.cu"]
 
 
 def _nvcc() -> str:

@@ -28,6 +28,7 @@ MIX_FLAG_SAE_EDIT_ONLY = 8
 MIX_FLAG_SLOT_CHAINS = 16
 MIX_FLAG_FP8_W_ENC = 32
 MIX_FLAG_FP8_ACT = 64
+MIX_DTYPE_F32, MIX_DTYPE_BF16, MIX_DTYPE_F16 = 0, 1, 2
 
 EXPORTS = [
     "mix_create", "mix_destroy", "mix_last_error", "mix_register_sae_weights", "mix_unregister_sae_weights",
@@ -35,6 +36,9 @@ EXPORTS = [
     "mix_set_slot_map", "mix_set_request_map", "mix_set_feature_out", "mix_apply", "mix_apply_conditional", "mix_apply_router", "mix_get_status",
     "mix_launches_per_apply", "mix_set_stage_events", "mix_debug_workspace", "mix_sae_apply_static",
     "mix_bench_param_update", "mix_set_pdl_mask", "mix_debug_phase_clocks",
+    "mix_router_topk", "mix_router_topk_grad", "mix_expert_order", "mix_expert_order_workspace", "mix_router_balance",
+    "mix_router_balance_workspace", "mix_router_balance_grad", "mix_quantize_rows", "mix_linear_int", "mix_linear_int_grouped",
+    "mix_linear_int_status", "mix_expert_combine",
 ]
 
 
@@ -114,9 +118,22 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
                                          C.c_char_p, ci]
     lib.mix_debug_workspace.argtypes = [vp, C.POINTER(vp), C.POINTER(vp), C.POINTER(C.c_longlong), C.POINTER(ci)]
     lib.mix_debug_phase_clocks.argtypes = [vp, C.POINTER(C.c_ulonglong)]
+    ll, err = C.c_longlong, [vp, C.c_char_p, ci]         # every call without a context ends in: stream, errbuf, errbuf_len
+    lib.mix_router_topk.argtypes = [vp, ci, ll, ci, ci, ci, ci, ci, vp, vp, vp] + err
+    lib.mix_router_topk_grad.argtypes = [vp, ci, ll, ci, ci, ci, ci, ci, vp, vp, vp, vp, ll] + err
+    lib.mix_expert_order_workspace.argtypes = [ll, ci]
+    lib.mix_expert_order.argtypes = [vp, ll, ci, vp, vp, vp, vp, ll] + err
+    lib.mix_router_balance_workspace.argtypes = [ci, ci, ci]
+    lib.mix_router_balance.argtypes = [vp, ci, ll, vp, ci, ci, ci, ci, vp, ci, vp, vp, vp, vp, vp, ll] + err
+    lib.mix_router_balance_grad.argtypes = [vp, ci, ll, vp, ci, ci, ci, ci, vp, ci, vp, vp, vp, vp, ll] + err
+    lib.mix_quantize_rows.argtypes = [vp, ci, ll, ci, vp, ci, ci, ci, vp, vp] + err
+    lib.mix_linear_int.argtypes = [vp, vp, ci, ci, vp, vp, ci, vp, vp, ci, ll] + err
+    lib.mix_linear_int_grouped.argtypes = [vp, vp, ci, ci, vp, vp, ci, ci, vp, vp, vp, ci, ll] + err
+    lib.mix_linear_int_status.argtypes = [C.POINTER(C.c_uint)] + err
+    lib.mix_expert_combine.argtypes = [vp, ci, ll, ci, vp, vp, ci, ci, ci, vp, ll] + err
     for name in EXPORTS:
         if name != "mix_last_error":
-            getattr(lib, name).restype = ci
+            getattr(lib, name).restype = ll if name.endswith("_workspace") and name != "mix_debug_workspace" else ci
     if path == _build.LIB_PATH:
         from . import _fastcall
         _lib, _fast = lib, _fastcall

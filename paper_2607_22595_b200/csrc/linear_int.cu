@@ -1,0 +1,533 @@
+// Products in 8-bit integers with a scale for each token and each output channel.
+//
+//   quantize_rows_kernel  codes[t, i] = round(127 x[t, i] / a_t), scale[t] = a_t / 127, a_t = max |x[t, :]|
+//   linear_int_kernel      y[t, n] = (sum_i codes[t, i] W[n, i]) scale[t] w_scale[n] + bias[n], the sum exact in 32-bit integers;
+//                         grouped: rows offsets[e] .. offsets[e + 1] go through weight set e
+//   combine_kernel        out[t, :] = sum_j weight[t, j] y[position[t, j], :]
+#include "op_common.cuh"
+#include "tc_common.cuh"
+
+using namespace mix;
+using namespace mix::tc;
+
+namespace {
+
+// ---------------------------------------------------------------------------------------------------- quantisation
+// A row's codes are the exact quotients 127 x / a rounded to the nearest, halves to the even one: x has 11 significant bits at
+// most, 127 x is exact in fp32, the quotient is never so close to a half that a correctly rounded division would cross it.  A
+// division costs more than the rest of the row's work, so the quotient comes from a multiplication by 127 / a and is divided
+// only where it lies within 2^-13 of a half (the multiplication is off by at most 127 * 2^-23).
+// A row that lies far from 1 is first scaled by a power of two, which is exact: neither 127 x nor 127 / a leaves fp32's range.
+template <typename T>
+__device__ __forceinline__ signed char code_of(float x, float inv, float a) {
+  float q = x * inv;
+  float r = rintf(q);
+  if (fabsf(fabsf(q - r) - 0.5f) < 0.000122f) r = rintf(__fdiv_rn(127.f * x, a));
+  return (signed char)(int)r;
+}
+
+constexpr int kQuantVecs = 4;                                  // 8-element vectors a thread keeps
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS < 128 ? 128 : THREADS)
+quantize_rows_kernel(const T* __restrict__ x, long long ld, int vec, int x_rows, const int* __restrict__ order, int div, int n_rows, int d,
+                     signed char* __restrict__ codes, float* __restrict__ scale) {
+  constexpr int kRows = THREADS < 128 ? 128 / THREADS : 1;     // rows a CTA takes
+  __shared__ float red[kRows == 1 ? THREADS / 32 : 1];
+  pdl_wait();
+  pdl_launch_dependents();
+  const int tid = threadIdx.x % THREADS;
+  const long long i = (long long)blockIdx.x * kRows + threadIdx.x / THREADS;
+  if (i >= n_rows) return;                                     // (whole warps; a CTA of one row has it)
+  long long src = i;
+  if (order) {
+    const int o = order[i];
+    src = o < 0 ? -1 : o / div;
+    if (src >= x_rows) src = -1;
+  }
+  const int n_vec = d / 8;                                     // (d is a multiple of 16)
+  uint2* out = reinterpret_cast<uint2*>(codes + i * d);
+  if (src < 0) {                                               // an entry without a token: zeros
+    for (int v = tid; v < n_vec; v += THREADS) out[v] = make_uint2(0u, 0u);
+    if (tid == 0) scale[i] = 0.f;
+    return;
+  }
+  const T* row = x + src * ld;
+  uint4 keep[kQuantVecs];
+  float a = 0.f;
+  bool bad = false;                                            // fmaxf drops NaN
+  auto fetch = [&](int v) -> uint4 {
+    if (vec) return *reinterpret_cast<const uint4*>(row + 8ll * v);
+    uint4 raw;
+    T* e = reinterpret_cast<T*>(&raw);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = row[8ll * v + j];
+    return raw;
+  };
+  auto look = [&](const uint4& raw) {
+    const T* e = reinterpret_cast<const T*>(&raw);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float f = fabsf(to_f32(e[j]));
+      a = fmaxf(a, f);
+      bad |= !(f <= 3.402823466e38f);
+    }
+  };
+#pragma unroll
+  for (int b = 0; b < kQuantVecs; ++b) {
+    const int v = tid + b * THREADS;
+    keep[b] = v < n_vec ? fetch(v) : make_uint4(0u, 0u, 0u, 0u);
+  }
+#pragma unroll
+  for (int b = 0; b < kQuantVecs; ++b) look(keep[b]);
+  for (int v = tid + kQuantVecs * THREADS; v < n_vec; v += THREADS) look(fetch(v));
+  if (bad) a = INFINITY;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
+  if (kRows == 1 && THREADS > 32) {
+    if ((tid & 31) == 0) red[tid >> 5] = a;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) a = fmaxf(a, red[w]);
+  }
+  if (!(a < INFINITY)) {                                       // a row with an infinity or a NaN: its products are NaN
+    for (int v = tid; v < n_vec; v += THREADS) out[v] = make_uint2(0u, 0u);
+    if (tid == 0) scale[i] = __int_as_float(0x7fc00000);
+    return;
+  }
+  const float pre = a > 1e30f ? 0x1p-64f : (a < 1e-30f ? 0x1p64f : 1.f);
+  const float as = a * pre, inv = as > 0.f ? 127.f / as : 0.f;
+  auto quantize = [&](const uint4& raw) -> uint2 {
+    const T* e = reinterpret_cast<const T*>(&raw);
+    uint2 c;
+    signed char* b = reinterpret_cast<signed char*>(&c);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) b[j] = code_of<T>(to_f32(e[j]) * pre, inv, as);
+    return c;
+  };
+  if (as == 0.f) {
+    for (int v = tid; v < n_vec; v += THREADS) out[v] = make_uint2(0u, 0u);
+  } else {
+#pragma unroll
+    for (int b = 0; b < kQuantVecs; ++b) {
+      const int v = tid + b * THREADS;
+      if (v < n_vec) out[v] = quantize(keep[b]);
+    }
+    for (int v = tid + kQuantVecs * THREADS; v < n_vec; v += THREADS) out[v] = quantize(fetch(v));
+  }
+  if (tid == 0) scale[i] = __fdiv_rn(a, 127.f);
+}
+
+// ---------------------------------------------------------------------------------------------------- the product
+// A tile is 128 output channels x NT tokens: the WEIGHTS are the matrix operand with 128 rows and the tokens the one with NT, so
+// that a few tokens (a decode step, an expert's share) make a narrow tile and not one of mostly empty rows.  Accumulators are
+// 32-bit integers in tensor memory, two of them, so that one tile is written out while the next is computed.
+constexpr int kTileCh = 128;                                   // output channels of a tile
+constexpr int kKBytes = 128;                                   // codes of a row in a stage: one swizzled 128-byte line
+constexpr int kGemmThreads = 192;                              // copies, tensor-core instructions, four warps of epilogue
+constexpr long long kI8WaitCycles = 4000000000ll;              // about two seconds
+
+__device__ unsigned g_i8_status;                               // MIX_STATUS_WAIT_TIMEOUT, until mix_linear_int_status reads it
+__device__ const long long g_i8_wait_cycles = kI8WaitCycles;
+
+template <int NT>
+struct GemmCfg {
+  static constexpr int kBoxRows = NT < 64 ? NT : 64;           // tokens of a copy
+  static constexpr int kABytes = kTileCh * kKBytes;
+  static constexpr int kStageBytes = kABytes + NT * kKBytes;
+  static constexpr int kStages = (200 * 1024) / kStageBytes < 12 ? (200 * 1024) / kStageBytes : 12;
+  static constexpr int kTmemCols = 2 * NT < 32 ? 32 : 2 * NT;
+  static constexpr int kSmem = kStages * kStageBytes + 1024;
+};
+
+struct GemmShared {
+  unsigned long long full[12], empty[12], acc_full[2], acc_empty[2];
+  unsigned tmem_base;
+  int abort_flag;
+  int row0[kOpMaxExperts + 1];                                 // rows of expert e: row0[e] .. row0[e + 1]
+  int tile0[kOpMaxExperts + 1];                                // tiles of expert e
+};
+
+// kind::i8: 32-bit integer accumulators, both operands signed, both K-major; K = 32 codes an instruction
+__host__ __device__ constexpr unsigned idesc_i8(int m, int n) {
+  return (2u << 4) | (1u << 7) | (1u << 10) | ((unsigned)(n >> 3) << 17) | ((unsigned)(m >> 4) << 24);
+}
+__device__ __forceinline__ void umma_i8(unsigned d_tmem, unsigned long long a, unsigned long long b, unsigned idesc, unsigned accumulate,
+                                        unsigned on) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 e, %5, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(on)
+      : "memory");
+}
+
+struct I8Tile {
+  int expert, ch0, row0, n_tok;
+};
+
+template <int NT>
+__device__ __forceinline__ I8Tile i8_tile(const GemmShared* sh, int tile, int& e) {
+  while (tile >= sh->tile0[e + 1]) ++e;                        // (a role's tiles only rise)
+  const int local = tile - sh->tile0[e], rows = sh->row0[e + 1] - sh->row0[e], tt = (rows + NT - 1) / NT;
+  I8Tile t;
+  t.expert = e;
+  t.ch0 = local / tt * kTileCh;                                // token tiles of the same channels are neighbours: W comes from DRAM once
+  const int tk = local % tt;
+  t.row0 = sh->row0[e] + tk * NT;
+  t.n_tok = min(NT, rows - tk * NT);
+  return t;
+}
+
+template <typename OutT, int NT>
+__global__ void __launch_bounds__(kGemmThreads, 1)
+linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x, const float* __restrict__ scale,
+                 const float* __restrict__ w_scale, const float* __restrict__ bias, const int* __restrict__ offsets, int n_rows, int K,
+                 int N, int E, OutT* __restrict__ out, long long ld_out) {
+  using Cfg = GemmCfg<NT>;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* ring = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  __shared__ GemmShared shared;
+  __shared__ float tok_scale[4][NT];                           // a copy per warp of the epilogue
+  GemmShared* sh = &shared;
+  const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < Cfg::kStages; ++s) {
+      mbar_init(smem_u32(&sh->full[s]), 1);
+      mbar_init(smem_u32(&sh->empty[s]), 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(smem_u32(&sh->acc_full[a]), 1);
+      mbar_init(smem_u32(&sh->acc_empty[a]), 4);
+    }
+    sh->abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) tmem_alloc(smem_u32(&sh->tmem_base), Cfg::kTmemCols);
+  pdl_wait();
+  pdl_launch_dependents();
+  const int ch_tiles = (N + kTileCh - 1) / kTileCh;
+  if (warp == 0) {                                             // the experts' rows and tiles; offsets that fall or leave the rows are held in
+    int row = 0, tiles = 0;
+    for (int e0 = 0; e0 < E; e0 += 32) {
+      const int e = e0 + lane;
+      int end = offsets ? (e < E ? min(max(offsets[e + 1], 0), n_rows) : 0) : n_rows;
+      int begin = offsets ? (e < E ? min(max(offsets[e], 0), n_rows) : 0) : 0;
+      if (e0 == 0) row = __shfl_sync(0xffffffffu, begin, 0);
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {                       // running maximum: never below an earlier offset
+        const int y = __shfl_up_sync(0xffffffffu, end, o);
+        if (lane >= o) end = max(end, y);
+      }
+      end = max(end, row);
+      int prev = __shfl_up_sync(0xffffffffu, end, 1);
+      if (lane == 0) prev = row;
+      int n = e < E ? (end - prev + NT - 1) / NT * ch_tiles : 0;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, n, o);
+        if (lane >= o) n += y;
+      }
+      if (e < E) {
+        sh->row0[e + 1] = end;
+        sh->tile0[e + 1] = tiles + n;
+        if (e == 0) {
+          sh->row0[0] = prev;
+          sh->tile0[0] = 0;
+        }
+      }
+      row = __shfl_sync(0xffffffffu, end, 31);
+      tiles += __shfl_sync(0xffffffffu, n, 31);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const unsigned tmem_base = (unsigned)uniform((int)sh->tmem_base);
+  const int total = uniform(sh->tile0[E]);
+  const int num_kb = (K + kKBytes - 1) / kKBytes;
+  const long long* cap = &g_i8_wait_cycles;
+
+  if (warp == 0) {
+    int stage = 0, e = 0;
+    unsigned phase = 0;
+    bool ok = true;
+    for (int tile = blockIdx.x; tile < total && ok; tile += gridDim.x) {
+      const I8Tile t = i8_tile<NT>(sh, tile, e);
+      const int boxes = uniform((t.n_tok + Cfg::kBoxRows - 1) / Cfg::kBoxRows);
+      const int wy = uniform(t.expert * N + t.ch0), xy = uniform(t.row0);      // (E * N rows of W fit in 31 bits: checked on the host)
+      const unsigned bytes = Cfg::kABytes + boxes * Cfg::kBoxRows * kKBytes;
+      for (int kb = 0; kb < num_kb; ++kb) {
+        if (!mbar_wait_bounded_warp(smem_u32(&sh->empty[stage]), phase ^ 1u, &sh->abort_flag, cap, &g_i8_status)) { ok = false; break; }
+        const unsigned bar = smem_u32(&sh->full[stage]), sa = smem_u32(ring + stage * Cfg::kStageBytes), on = elect_one();
+        mbar_expect_tx(bar, bytes, on);
+        tma_load_2d(sa, &tmap_w, kb * kKBytes, wy, bar, on);
+        for (int b = 0; b < boxes; ++b)
+          tma_load_2d(sa + Cfg::kABytes + b * Cfg::kBoxRows * kKBytes, &tmap_x, kb * kKBytes, xy + b * Cfg::kBoxRows, bar, on);
+        if (++stage == Cfg::kStages) { stage = 0; phase ^= 1u; }
+      }
+    }
+  } else if (warp == 1) {
+    int stage = 0, e = 0;
+    unsigned phase = 0, acc = 0, acc_phase = 0;
+    bool ok = true;
+    for (int tile = blockIdx.x; tile < total && ok; tile += gridDim.x) {
+      const I8Tile t = i8_tile<NT>(sh, tile, e);
+      const unsigned idesc = (unsigned)uniform((int)idesc_i8(kTileCh, (t.n_tok + 15) & ~15));
+      if (!mbar_wait_bounded_warp(smem_u32(&sh->acc_empty[acc]), acc_phase ^ 1u, &sh->abort_flag, cap, &g_i8_status)) break;
+      tc_fence_after();
+      const unsigned d_tmem = tmem_base + acc * NT;
+      for (int kb = 0; kb < num_kb; ++kb) {
+        if (!mbar_wait_bounded_warp(smem_u32(&sh->full[stage]), phase, &sh->abort_flag, cap, &g_i8_status)) { ok = false; break; }
+        tc_fence_after();
+        const unsigned sa = smem_u32(ring + stage * Cfg::kStageBytes);
+        const unsigned long long da = umma_desc(sa), db = umma_desc(sa + Cfg::kABytes);
+        const unsigned on = elect_one();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) umma_i8(d_tmem, da + 2ull * k, db + 2ull * k, idesc, (unsigned)((kb | k) != 0), on);
+        umma_commit(smem_u32(&sh->empty[stage]), on);
+        if (++stage == Cfg::kStages) { stage = 0; phase ^= 1u; }
+      }
+      if (!ok) break;
+      umma_commit(smem_u32(&sh->acc_full[acc]), elect_one());
+      acc ^= 1u;
+      if (acc == 0) acc_phase ^= 1u;
+    }
+  } else {
+    const int q = warp & 3;                                    // tensor-memory lanes this warp may read
+    int e = 0;
+    unsigned acc = 0, acc_phase = 0;
+    float* my_scale = tok_scale[q];
+    for (int tile = blockIdx.x; tile < total; tile += gridDim.x) {
+      const I8Tile t = i8_tile<NT>(sh, tile, e);
+      const int ch = t.ch0 + q * 32 + lane;
+      const bool valid = ch < N;
+      const float ws = valid ? w_scale[(long long)t.expert * N + ch] : 0.f;
+      const float bs = valid && bias ? bias[(long long)t.expert * N + ch] : 0.f;
+      __syncwarp();
+      for (int i = lane; i < t.n_tok; i += 32) my_scale[i] = scale[t.row0 + i];
+      __syncwarp();
+      if (!mbar_wait_bounded_warp(smem_u32(&sh->acc_full[acc]), acc_phase, &sh->abort_flag, cap, &g_i8_status)) break;
+      tc_fence_after();
+      const unsigned taddr = tmem_base + acc * NT + ((unsigned)(q * 32) << 16);
+      OutT* dst = out + (long long)t.row0 * ld_out + ch;
+      for (int c0 = 0; c0 < t.n_tok; c0 += 32) {
+        float v[32];
+        __syncwarp();
+        tmem_ld32(taddr + c0, v);
+        if (valid) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (c0 + i < t.n_tok) dst[(c0 + i) * ld_out] = from_f32<OutT>(fmaf((float)__float_as_int(v[i]) * my_scale[c0 + i], ws, bs));
+        }
+      }
+      tc_fence_before();
+      if (lane == 0) mbar_arrive(smem_u32(&sh->acc_empty[acc]));
+      acc ^= 1u;
+      if (acc == 0) acc_phase ^= 1u;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (sh->abort_flag) {                                        // copies in flight land before shared memory is released
+    const long long t0 = clock64();
+    while (clock64() - t0 < 2000000ll) __nanosleep(1000);
+  }
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, Cfg::kTmemCols);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------- the sum over experts
+template <typename T>
+__global__ void __launch_bounds__(256)
+combine_kernel(const T* __restrict__ y, long long ld_y, int y_rows, const float* __restrict__ weights, const int* __restrict__ position, int T_rows,
+               int k, int N, T* __restrict__ out, long long ld_out, int vec) {
+  __shared__ float w[kOpMaxTopk];
+  __shared__ int at[kOpMaxTopk];
+  pdl_wait();
+  pdl_launch_dependents();
+  const long long t = blockIdx.x;
+  if (threadIdx.x < k) {
+    const int p = position[t * k + threadIdx.x];
+    at[threadIdx.x] = p >= 0 && p < y_rows ? p : -1;
+    w[threadIdx.x] = weights[t * k + threadIdx.x];
+  }
+  __syncthreads();
+  constexpr int VW = RowVec<T>::VW;
+  const int n_vec = vec ? N / VW : 0;
+  for (int v = blockIdx.y * 256 + threadIdx.x; v < n_vec; v += gridDim.y * 256) {
+    float acc[VW];
+#pragma unroll
+    for (int i = 0; i < VW; ++i) acc[i] = 0.f;
+    for (int j = 0; j < k; ++j) {
+      if (at[j] < 0) continue;
+      const uint4 raw = *reinterpret_cast<const uint4*>(y + at[j] * ld_y + (long long)VW * v);
+      const T* e = reinterpret_cast<const T*>(&raw);
+#pragma unroll
+      for (int i = 0; i < VW; ++i) acc[i] = fmaf(w[j], to_f32(e[i]), acc[i]);
+    }
+    uint4 raw;
+    T* e = reinterpret_cast<T*>(&raw);
+#pragma unroll
+    for (int i = 0; i < VW; ++i) e[i] = from_f32<T>(acc[i]);
+    *reinterpret_cast<uint4*>(out + t * ld_out + (long long)VW * v) = raw;
+  }
+  for (int c = n_vec * VW + blockIdx.y * 256 + threadIdx.x; c < N; c += gridDim.y * 256) {
+    float acc = 0.f;
+    for (int j = 0; j < k; ++j)
+      if (at[j] >= 0) acc = fmaf(w[j], to_f32(y[at[j] * ld_y + c]), acc);
+    out[t * ld_out + c] = from_f32<T>(acc);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------- host side
+struct Gemm {
+  const void* codes;
+  const float* scale;
+  const void* w;
+  const float* w_scale;
+  const float* bias;
+  const int* offsets;
+  int n_rows, K, N, E;
+  void* out;
+  long long ld_out;
+};
+
+template <typename OutT, int NT>
+cudaError_t gemm_launch(const Gemm& g, int dev, int n_sms, cudaStream_t s) {
+  using Cfg = GemmCfg<NT>;
+  static std::atomic<int> ready[kOpDevices];
+  if (!ready[dev].load(std::memory_order_relaxed)) {
+    const cudaError_t e = cudaFuncSetAttribute(linear_int_kernel<OutT, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem);
+    if (e != cudaSuccess) return e;
+    ready[dev].store(1, std::memory_order_relaxed);
+  }
+  CUtensorMap tw, tx;
+  if (make_tmap_i8(&tw, g.w, (unsigned long long)g.E * g.N, g.K, kTileCh) != MIX_OK || make_tmap_i8(&tx, g.codes, g.n_rows, g.K, Cfg::kBoxRows) != MIX_OK)
+    return cudaErrorInvalidValue;
+  const long long tok_tiles = (long long)g.n_rows / NT + (g.E < g.n_rows ? g.E : g.n_rows);      // at most, however the rows fall
+  const long long most = (g.E == 1 ? (g.n_rows + NT - 1) / NT : tok_tiles) * ((g.N + kTileCh - 1) / kTileCh);
+  const int grid = (int)(most < n_sms ? most : n_sms);
+  return launch_pdl(kPdlHook, linear_int_kernel<OutT, NT>, dim3(grid), dim3(kGemmThreads), Cfg::kSmem, s, tw, tx, g.scale, g.w_scale, g.bias,
+                    g.offsets, g.n_rows, g.K, g.N, g.E, static_cast<OutT*>(g.out), g.ld_out);
+}
+
+template <typename OutT>
+cudaError_t gemm_pick(const Gemm& g, int dev, int n_sms, cudaStream_t s) {
+  const int share = (g.n_rows + g.E - 1) / g.E;
+  if (share <= 32) return gemm_launch<OutT, 32>(g, dev, n_sms, s);
+  if (share <= 64) return gemm_launch<OutT, 64>(g, dev, n_sms, s);
+  if (share <= 128) return gemm_launch<OutT, 128>(g, dev, n_sms, s);
+  return gemm_launch<OutT, 256>(g, dev, n_sms, s);
+}
+
+int gemm_call(const Gemm& g, int dtype, void* stream, char* errbuf, int errbuf_len) {
+  if (op_elem_size(dtype) == 0) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "dtype %d is no MIX_DTYPE_*", dtype);
+  if (g.n_rows < 0) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "n_rows %d is negative", g.n_rows);
+  if (g.K < 16 || g.K > MIX_I8_MAX_K) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "K %d outside [16, %d]", g.K, MIX_I8_MAX_K);
+  if (g.K % 16) MIX_OP_FAIL(MIX_ERR_UNSUPPORTED, "K %d is not a multiple of 16", g.K);
+  if (g.N < 1) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "N %d is below 1", g.N);
+  if (g.E < 1 || g.E > kOpMaxExperts) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "n_experts %d outside [1, %d]", g.E, kOpMaxExperts);
+  if ((long long)g.E * g.N > 0x7fffff00ll) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "%lld rows of W", (long long)g.E * g.N);
+  const long long tiles = ((long long)g.n_rows / 32 + g.E) * ((g.N + kTileCh - 1) / kTileCh);
+  if (tiles > 0x7fffffffll) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "n_rows %d x N %d has too many tiles", g.n_rows, g.N);
+  if (g.ld_out < g.N) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "row stride %lld of the output is below N %d", g.ld_out, g.N);
+  if (g.n_rows == 0) return MIX_OK;
+  if (!g.codes || !g.scale || !g.w || !g.w_scale || !g.out) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "codes, scale, W, w_scale and out are required");
+  if (((uintptr_t)g.codes | (uintptr_t)g.w) & 15u) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "codes and W must be 16-byte aligned");
+  int dev, n_sms;
+  MIX_OP_CUDA(op_device(&dev, &n_sms));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (dtype == MIX_DTYPE_F32) MIX_OP_CUDA(gemm_pick<float>(g, dev, n_sms, s));
+  else if (dtype == MIX_DTYPE_BF16) MIX_OP_CUDA(gemm_pick<__nv_bfloat16>(g, dev, n_sms, s));
+  else MIX_OP_CUDA(gemm_pick<__half>(g, dev, n_sms, s));
+  return MIX_OK;
+}
+
+template <typename T>
+cudaError_t quantize_launch(const void* x, long long ld, int x_rows, const int* order, int div, int n_rows, int d, signed char* codes,
+                            float* scale, cudaStream_t s) {
+  const int vec = (((uintptr_t)x | (uintptr_t)(ld * 2)) & 15u) == 0;
+  const T* xt = static_cast<const T*>(x);
+  if (d <= 1024)                                               // a warp holds the row
+    return launch_pdl(kPdlHook, quantize_rows_kernel<T, 32>, dim3((unsigned)((n_rows + 3ll) / 4)), dim3(128), 0, s, xt, ld, vec, x_rows, order, div,
+                      n_rows, d, codes, scale);
+  if (d <= 4096)
+    return launch_pdl(kPdlHook, quantize_rows_kernel<T, 128>, dim3((unsigned)n_rows), dim3(128), 0, s, xt, ld, vec, x_rows, order, div, n_rows, d,
+                      codes, scale);
+  return launch_pdl(kPdlHook, quantize_rows_kernel<T, 256>, dim3((unsigned)n_rows), dim3(256), 0, s, xt, ld, vec, x_rows, order, div, n_rows, d,
+                    codes, scale);
+}
+
+template <typename T>
+cudaError_t combine_launch(const void* y, long long ld_y, int y_rows, const float* weights, const int* position, int T_rows, int k, int N,
+                           void* out, long long ld_out, int n_sms, cudaStream_t s) {
+  const int vec = (((uintptr_t)y | (uintptr_t)out | (uintptr_t)(ld_y * (long long)sizeof(T)) | (uintptr_t)(ld_out * (long long)sizeof(T))) & 15u) == 0;
+  const int pieces = vec ? (N / RowVec<T>::VW + 255) / 256 : (N + 255) / 256;
+  int gy = 1;                                                  // few tokens: their columns are dealt to several CTAs
+  while (gy < pieces && gy < 64 && (long long)T_rows * gy < 2 * n_sms) gy *= 2;
+  return launch_pdl(kPdlHook, combine_kernel<T>, dim3((unsigned)T_rows, gy), dim3(256), 0, s, static_cast<const T*>(y), ld_y, y_rows, weights,
+                    position, T_rows, k, N, static_cast<T*>(out), ld_out, vec);
+}
+
+}  // namespace
+
+extern "C" int mix_quantize_rows(const void* x, int dtype, long long ld, int x_rows, const int* order, int k, int n_rows, int d,
+                                    signed char* codes, float* scale, void* stream, char* errbuf, int errbuf_len) {
+  if (dtype != MIX_DTYPE_BF16 && dtype != MIX_DTYPE_F16) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "dtype %d is neither bf16 nor fp16", dtype);
+  if (n_rows < 0 || x_rows < 0) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "%d rows of %d", n_rows, x_rows);
+  if (d < 16 || d > MIX_I8_MAX_K) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "d %d outside [16, %d]", d, MIX_I8_MAX_K);
+  if (d % 16) MIX_OP_FAIL(MIX_ERR_UNSUPPORTED, "d %d is not a multiple of 16", d);
+  if (ld < d) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "row stride %lld is below d %d", ld, d);
+  if (order && k < 1) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "k %d is below 1", k);
+  if (!order && n_rows != x_rows) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "without an order the %d rows of x make as many, not %d", x_rows, n_rows);
+  if (n_rows == 0) return MIX_OK;
+  if ((!x && x_rows > 0) || !codes || !scale) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "x, codes and scale are required");
+  if ((uintptr_t)codes & 15u) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "codes must be 16-byte aligned");
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (dtype == MIX_DTYPE_BF16) MIX_OP_CUDA(quantize_launch<__nv_bfloat16>(x, ld, x_rows, order, k, n_rows, d, codes, scale, s));
+  else MIX_OP_CUDA(quantize_launch<__half>(x, ld, x_rows, order, k, n_rows, d, codes, scale, s));
+  return MIX_OK;
+}
+
+extern "C" int mix_linear_int(const signed char* codes, const float* scale, int T, int K, const signed char* W, const float* w_scale, int N,
+                             const float* bias, void* out, int out_dtype, long long ld_out, void* stream, char* errbuf, int errbuf_len) {
+  return gemm_call(Gemm{codes, scale, W, w_scale, bias, nullptr, T, K, N, 1, out, ld_out}, out_dtype, stream, errbuf, errbuf_len);
+}
+
+extern "C" int mix_linear_int_grouped(const signed char* codes, const float* scale, int n_rows, int K, const signed char* W, const float* w_scale,
+                                     int n_experts, int N, const int* offsets, const float* bias, void* out, int out_dtype, long long ld_out,
+                                     void* stream, char* errbuf, int errbuf_len) {
+  if (!offsets) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "offsets is NULL");
+  return gemm_call(Gemm{codes, scale, W, w_scale, bias, offsets, n_rows, K, N, n_experts, out, ld_out}, out_dtype, stream, errbuf, errbuf_len);
+}
+
+extern "C" int mix_linear_int_status(unsigned* bits, void* stream, char* errbuf, int errbuf_len) {
+  if (!bits) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "bits is NULL");
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const unsigned zero = 0;
+  MIX_OP_CUDA(cudaMemcpyFromSymbolAsync(bits, g_i8_status, sizeof(unsigned), 0, cudaMemcpyDeviceToHost, s));
+  MIX_OP_CUDA(cudaMemcpyToSymbolAsync(g_i8_status, &zero, sizeof(unsigned), 0, cudaMemcpyHostToDevice, s));
+  MIX_OP_CUDA(cudaStreamSynchronize(s));
+  return MIX_OK;
+}
+
+extern "C" int mix_expert_combine(const void* y, int dtype, long long ld_y, int y_rows, const float* weights, const int* position, int T, int k,
+                                  int N, void* out, long long ld_out, void* stream, char* errbuf, int errbuf_len) {
+  if (op_elem_size(dtype) == 0) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "dtype %d is no MIX_DTYPE_*", dtype);
+  if (T < 0 || y_rows < 0) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "%d tokens, %d rows of y", T, y_rows);
+  if (k < 1 || k > kOpMaxTopk) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "k %d outside [1, %d]", k, kOpMaxTopk);
+  if (N < 1) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "N %d is below 1", N);
+  if (ld_y < N || ld_out < N) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "row strides %lld, %lld below N %d", ld_y, ld_out, N);
+  if (T == 0) return MIX_OK;
+  if ((!y && y_rows > 0) || !weights || !position || !out) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "y, weights, position and out are required");
+  int dev, n_sms;
+  MIX_OP_CUDA(op_device(&dev, &n_sms));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (dtype == MIX_DTYPE_F32) MIX_OP_CUDA(combine_launch<float>(y, ld_y, y_rows, weights, position, T, k, N, out, ld_out, n_sms, s));
+  else if (dtype == MIX_DTYPE_BF16) MIX_OP_CUDA(combine_launch<__nv_bfloat16>(y, ld_y, y_rows, weights, position, T, k, N, out, ld_out, n_sms, s));
+  else MIX_OP_CUDA(combine_launch<__half>(y, ld_y, y_rows, weights, position, T, k, N, out, ld_out, n_sms, s));
+  return MIX_OK;
+}

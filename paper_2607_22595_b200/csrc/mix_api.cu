@@ -289,6 +289,10 @@ int make_tmap(CUtensorMap* out, const void* base, unsigned long long rows, int d
   return r == CUDA_SUCCESS ? MIX_OK : MIX_ERR_CUDA;
 }
 
+int make_tmap_i8(CUtensorMap* out, const void* base, unsigned long long rows, unsigned long long width, int box_rows) {
+  return load_encode_fn() == MIX_OK ? make_tmap_e4m3(out, base, rows, width, box_rows) : MIX_ERR_CUDA;
+}
+
 static int g_pdl_mask = -1;        // -1: not yet read from the environment
 int pdl_mask() {
   // default: not the full encode pass -- measured, its early-resident CTAs cost config 3 about 7 us

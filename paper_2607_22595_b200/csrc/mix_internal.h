@@ -311,6 +311,8 @@ cudaError_t launch_front(const Ctx* c, __nv_bfloat16* hidden, int T, cudaStream_
 int front_chunks(int T_max);       // chunks of token rows the front kernel classifies: sizes d_front_counts / d_front_sync
 // bf16 [rows, d] row-major, boxes of 64 columns x box_rows rows, 128-byte swizzle; host work only
 int make_tmap(CUtensorMap* out, const void* base, unsigned long long rows, int d, int box_rows);
+// 8-bit codes [rows, width] row-major, boxes of 128 columns x box_rows rows, 128-byte swizzle; host work only
+int make_tmap_i8(CUtensorMap* out, const void* base, unsigned long long rows, unsigned long long width, int box_rows);
 cudaError_t launch_encode_simt(const Ctx* c, cudaStream_t s);
 cudaError_t launch_encode_tc(const Ctx* c, int mode, bool pair, cudaStream_t s);   // 0: all tiles; 1: flagged row tiles -> Z
 inline int cand_tiles_for(long long d_sae_max, int n_sms) {   // Ctx::cand_tiles

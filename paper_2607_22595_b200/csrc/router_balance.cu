@@ -1,0 +1,456 @@
+// How evenly a router spreads the tokens of each request over its experts, and the loss on it.
+//
+// For a segment s of rows (a request), n_s of which name an expert, with C_e = how often they name expert e:
+//   f_e = C_e / sum C        P_e = mean over the n_s rows of p_te        L_s = E sum_e f_e P_e
+//   dL_s / dx_tj = E / n_s  p_tj (f_j - sum_e f_e p_te)  [(1 - sigmoid(x_tj))  where the scores are sigmoids]
+// f counts, so no gradient passes through it.
+//
+// Forward: one pass over the logits.  A CTA (unit u) takes a run of rows, walks the segments that the run touches and leaves
+// what it saw of each in slot u + s of the partial sums -- along the runs and segments either u or s goes up by one at every
+// step, so no two share a slot, and which row is added where never depends on timing.  A second launch adds the slots up, a
+// cluster of CTAs per segment where a segment has many.  Both add in a fixed order.
+// Backward: one pass over the logits, a warp per run of rows.
+#include "op_common.cuh"
+#include "tc_common.cuh"
+
+using namespace mix;
+
+namespace {
+
+constexpr int kUnitWarps = 8;              // warps of a unit where requests are long
+constexpr int kFinThreads = 512;
+constexpr int kFinCluster = 8;
+
+// Offset i of n_seg segments, in [0, T] whatever stands in the table; without a table all rows are one segment.
+__device__ __forceinline__ int seg_at(const int* __restrict__ seg, int i, int T) { return seg ? min(max(seg[i], 0), T) : (i == 0 ? 0 : T); }
+
+// The last segment that begins at or before row r (0 where none does), found by a whole warp: 32 probes a step.
+__device__ __forceinline__ int seg_of_row(const int* __restrict__ seg, int n_seg, int T, int r, int lane) {
+  int lo = 0, n = n_seg;                                       // the answer is in [lo, lo + n)
+  while (n > 1) {
+    const int step = (n + 31) / 32, at = lo + lane * step;
+    const unsigned ok = __ballot_sync(0xffffffffu, lane * step < n && seg_at(seg, at, T) <= r);
+    const int i = ok ? 31 - __clz(ok) : 0;
+    n = min(step, n - i * step);
+    lo += i * step;
+  }
+  return lo;
+}
+
+// Probabilities of a row held by G lanes, in place; rows that are off become zeros.
+template <typename T, int G, int V>
+__device__ __forceinline__ void probabilities(int act, bool on, float (&x)[V]) {
+  float top = x[0];
+#pragma unroll
+  for (int v = 1; v < V; ++v) top = fmaxf(top, x[v]);
+  top = group_max<G>(top);
+  float total = 0.f;
+  if (act == MIX_ACT_SOFTMAX) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      x[v] = score_softmax(x[v], top);
+      total += x[v];
+    }
+  } else {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      x[v] = score_sigmoid(x[v], top);
+      total += x[v];
+    }
+  }
+  total = group_sum<G>(total);
+  const float inv = on && total > 0.f ? 1.f / total : 0.f;
+#pragma unroll
+  for (int v = 0; v < V; ++v) x[v] *= inv;
+}
+
+template <typename T, int G, int V, int W>
+__global__ void __launch_bounds__(32 * W)
+balance_kernel(const T* __restrict__ logits, long long ld, int vec, const int* __restrict__ idx, int T_rows, int E, int k, int act,
+               const int* __restrict__ seg, int n_seg, int unit_rows, float* __restrict__ part_p, int* __restrict__ part_c,
+               int* __restrict__ part_n) {
+  constexpr int R = 32 / G;                                    // rows a warp holds
+  __shared__ int hist[G * V];
+  __shared__ float sum_p[W][G * V];
+  __shared__ int sum_n[W];
+  pdl_wait();
+  pdl_launch_dependents();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane & (G - 1), unit = blockIdx.x;
+  const int r0 = unit * unit_rows, r1 = min(T_rows, r0 + unit_rows);
+  for (int e = threadIdx.x; e < G * V; e += 32 * W) hist[e] = 0;
+  if (W > 1) __syncthreads(); else __syncwarp();
+  for (int s = seg_of_row(seg, n_seg, T_rows, r0, lane); s < n_seg; ++s) {
+    const int a = max(seg_at(seg, s, T_rows), r0), b = min(seg_at(seg, s + 1, T_rows), r1);
+    if (a >= r1) break;
+    if (a >= b) continue;
+    float acc[V];
+    int rows = 0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) acc[v] = 0.f;
+    for (int base = a + warp * R; base < b; base += W * R) {   // (all lanes of a warp: a row of no segment is a row that is off)
+      const int t = base + lane / G;
+      bool named = false;
+      float x[V];
+      if (t < b) {
+        load_row<T, G, V>(logits + t * ld, E, sub, vec != 0, x);
+        for (int j = sub; j < k; j += G) {
+          const int i = idx[(long long)t * k + j];
+          if ((unsigned)i < (unsigned)E) {
+            atomicAdd(&hist[i], 1);
+            named = true;
+          }
+        }
+      } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = -INFINITY;
+      }
+      const unsigned votes = __ballot_sync(0xffffffffu, named);
+      const bool on = G == 32 ? votes != 0u : ((votes >> (lane & ~(G - 1))) & ((1u << (G & 31)) - 1u)) != 0u;
+      rows += on && sub == 0;
+      probabilities<T, G, V>(act, on, x);
+#pragma unroll
+      for (int v = 0; v < V; ++v) acc[v] += x[v];
+    }
+    // this segment's share of the unit
+#pragma unroll
+    for (int o = G; o < 32; o <<= 1) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) acc[v] += __shfl_xor_sync(0xffffffffu, acc[v], o);
+    }
+    rows = __reduce_add_sync(0xffffffffu, rows);
+    if (lane < G) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) sum_p[warp][row_col<T, G>(v, sub)] = acc[v];
+    }
+    if (lane == 0) sum_n[warp] = rows;
+    if (W > 1) __syncthreads(); else __syncwarp();
+    const size_t slot = (size_t)(unit + s);
+    for (int e = threadIdx.x; e < E; e += 32 * W) {
+      float p = sum_p[0][e];
+#pragma unroll
+      for (int w = 1; w < W; ++w) p += sum_p[w][e];
+      part_p[slot * E + e] = p;
+      part_c[slot * E + e] = hist[e];
+      hist[e] = 0;
+    }
+    if (threadIdx.x == 0) {
+      int n = sum_n[0];
+#pragma unroll
+      for (int w = 1; w < W; ++w) n += sum_n[w];
+      part_n[slot] = n;
+    }
+    if (W > 1) __syncthreads(); else __syncwarp();
+  }
+}
+
+// One segment per cluster: CTA r of the cluster adds up the r-th part of the segment's slots, CTA 0 puts the parts together.
+// Sums in 64 bits: there are few, and a long request has thousands of slots.
+__global__ void __launch_bounds__(kFinThreads)
+balance_finish_kernel(const float* __restrict__ part_p, const int* __restrict__ part_c, const int* __restrict__ part_n, int T_rows, int E,
+                      const int* __restrict__ seg, int unit_rows, int cluster, float* __restrict__ loss, int* __restrict__ counts,
+                      float* __restrict__ mean_p, int* __restrict__ rows_out) {
+  __shared__ double sp[kOpMaxExperts];
+  __shared__ int sc[kOpMaxExperts];
+  __shared__ double red[kFinThreads / 32];
+  __shared__ long long red_c[kFinThreads / 32];
+  __shared__ int sn;
+  __shared__ double lane_p[kFinThreads];
+  __shared__ int lane_c[kFinThreads];
+  pdl_wait();
+  pdl_launch_dependents();
+  const int s = blockIdx.x / cluster, rank = blockIdx.x - s * cluster, tid = threadIdx.x;
+  const int a = seg_at(seg, s, T_rows), b = seg_at(seg, s + 1, T_rows);
+  int u0 = 0, u1 = 0;                                          // units that the segment touches
+  if (a < b) {
+    u0 = a / unit_rows;
+    u1 = (b - 1) / unit_rows + 1;
+  }
+  const int each = (u1 - u0 + cluster - 1) / cluster;
+  const int v0 = min(u1, u0 + rank * each), v1 = min(u1, v0 + each);
+  if (tid == 0) sn = 0;
+  __syncthreads();
+  {
+    int n = 0;
+    for (int u = v0 + tid; u < v1; u += kFinThreads) n += part_n[u + s];
+    n = __reduce_add_sync(0xffffffffu, n);
+    if ((tid & 31) == 0 && n) atomicAdd(&sn, n);
+  }
+  const int wide = min((E + 31) & ~31, kFinThreads), lanes = kFinThreads / wide;    // E <= 512 = kFinThreads: one pass
+  const int e = tid % wide, part = tid / wide;
+  double p = 0.0;
+  int c = 0;
+  if (part < lanes && e < E) {
+#pragma unroll 4
+    for (int u = v0 + part; u < v1; u += lanes) {
+      p += (double)part_p[(size_t)(u + s) * E + e];
+      c += part_c[(size_t)(u + s) * E + e];
+    }
+  }
+  lane_p[tid] = p;
+  lane_c[tid] = c;
+  __syncthreads();
+  if (tid < wide && e < E) {
+    for (int i = 1; i < lanes; ++i) {
+      p += lane_p[i * wide + tid];
+      c += lane_c[i * wide + tid];
+    }
+    sp[e] = p;
+    sc[e] = c;
+  }
+  if (cluster > 1) tc::cluster_sync_all(); else __syncthreads();
+  if (rank == 0) {
+    int n = sn;
+    for (int r = 1; r < cluster; ++r) {
+      int x;
+      asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(x) : "r"(tc::mapa_cluster(tc::smem_u32(&sn), r)));
+      n += x;
+    }
+    double fp = 0.0;
+    long long total = 0;
+    if (tid < E) {
+      p = sp[tid];
+      c = sc[tid];
+      for (int r = 1; r < cluster; ++r) {
+        double x;
+        int y;
+        asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(x) : "r"(tc::mapa_cluster(tc::smem_u32(&sp[tid]), r)));
+        asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(y) : "r"(tc::mapa_cluster(tc::smem_u32(&sc[tid]), r)));
+        p += x;
+        c += y;
+      }
+      p = n > 0 ? p / n : 0.0;
+      counts[(size_t)s * E + tid] = c;
+      mean_p[(size_t)s * E + tid] = (float)p;
+      fp = p * c;
+      total = c;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      fp += __shfl_xor_sync(0xffffffffu, fp, o);
+      total += __shfl_xor_sync(0xffffffffu, total, o);
+    }
+    if ((tid & 31) == 0) {
+      red[tid >> 5] = fp;
+      red_c[tid >> 5] = total;
+    }
+    __syncthreads();
+    if (tid == 0) {
+      for (int w = 1; w < kFinThreads / 32; ++w) {
+        fp += red[w];
+        total += red_c[w];
+      }
+      loss[s] = total > 0 ? (float)(E * fp / (double)total) : 0.f;
+      rows_out[s] = n;
+    }
+  }
+  if (cluster > 1) tc::cluster_sync_all();                     // the parts stay until they have been read
+}
+
+template <typename T, int G, int V>
+__global__ void __launch_bounds__(256)
+balance_grad_kernel(const T* __restrict__ logits, long long ld, int vec, const int* __restrict__ idx, int T_rows, int E, int k, int act,
+                    const int* __restrict__ seg, int n_seg, const int* __restrict__ counts, const int* __restrict__ rows,
+                    const float* __restrict__ d_loss, int warp_rows, T* __restrict__ d_logits, long long ld_d, int vec_d) {
+  constexpr int R = 32 / G;
+  pdl_wait();
+  pdl_launch_dependents();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane & (G - 1);
+  const long long run = ((long long)blockIdx.x * 8 + warp) * warp_rows;
+  if (run >= T_rows) return;                                   // (whole warps)
+  const int r0 = (int)run, r1 = (int)min((long long)T_rows, run + warp_rows);
+  const int s_first = seg_of_row(seg, n_seg, T_rows, r0, lane);
+  int at = r0;                                                 // rows in front of `at` are done
+  for (int s = s_first; at < r1; ++s) {
+    // rows [at, b) belong to segment s; what no segment covers, in front of the first or behind the last, gets zeros
+    const bool behind = s >= n_seg;
+    const int a = behind ? r1 : min(max(seg_at(seg, s, T_rows), at), r1);
+    const int b = behind ? r1 : min(max(seg_at(seg, s + 1, T_rows), a), r1);
+    float f[V];
+    float coef = 0.f;
+    if (a < b) {
+      long long total = 0;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int c = row_col<T, G>(v, sub);
+        const int n = c < E ? counts[(size_t)s * E + c] : 0;
+        f[v] = (float)n;
+        total += n;
+      }
+#pragma unroll
+      for (int o = 1; o < G; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+      const int n = rows[s];
+      coef = n > 0 ? d_loss[s] * (float)E / (float)n : 0.f;
+      const float inv = total > 0 ? 1.f / (float)total : 0.f;
+#pragma unroll
+      for (int v = 0; v < V; ++v) f[v] *= inv;
+    } else {
+#pragma unroll
+      for (int v = 0; v < V; ++v) f[v] = 0.f;
+    }
+    for (int base = at; base < b; base += R) {
+      const int t = base + lane / G;
+      const bool in = t < b, live = in && t >= a;
+      bool named = false;
+      float x[V], p[V];
+      if (live) {
+        load_row<T, G, V>(logits + t * ld, E, sub, vec != 0, x);
+        for (int j = sub; j < k; j += G) named |= (unsigned)idx[(long long)t * k + j] < (unsigned)E;
+      } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = -INFINITY;
+      }
+      const unsigned votes = __ballot_sync(0xffffffffu, named);
+      const bool on = G == 32 ? votes != 0u : ((votes >> (lane & ~(G - 1))) & ((1u << (G & 31)) - 1u)) != 0u;
+#pragma unroll
+      for (int v = 0; v < V; ++v) p[v] = x[v];
+      probabilities<T, G, V>(act, on, p);
+      float dot = 0.f;
+#pragma unroll
+      for (int v = 0; v < V; ++v) dot += f[v] * p[v];
+      dot = group_sum<G>(dot);
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        float d = coef * (p[v] * (f[v] - dot));
+        if (act == MIX_ACT_SIGMOID) d *= sigmoidf(-x[v]);
+        p[v] = on && p[v] > 0.f ? d : 0.f;                     // (also where the factors are not finite: a NaN in d_loss of rows that are off)
+      }
+      if (in) store_row<T, G, V>(d_logits + t * ld_d, E, sub, vec_d != 0, p);
+    }
+    at = b;
+  }
+}
+
+struct Plan {
+  int warps, unit_rows, units, cluster;
+  long long slots;
+};
+// Units of eight warps and at least 64 rows, six a SM at most, where the average request has 64 rows or more; where requests
+// are short (decode steps: one row each) a unit is one warp with 32 rows, and no barrier stands between two requests.
+Plan plan(int T, int n_seg, int n_sms) {
+  Plan p;
+  p.warps = T / n_seg >= 64 ? kUnitWarps : 1;
+  if (p.warps == kUnitWarps) {
+    p.unit_rows = (T + 6 * n_sms - 1) / (6 * n_sms);
+    if (p.unit_rows < 64) p.unit_rows = 64;
+  } else {
+    p.unit_rows = 32;
+  }
+  p.units = T > 0 ? (T + p.unit_rows - 1) / p.unit_rows : 0;
+  p.slots = (long long)p.units + n_seg;
+  p.cluster = p.units / n_seg >= 32 ? kFinCluster : 1;
+  return p;
+}
+long long workspace_bytes_of(const Plan& p, int E) { return p.slots * (8ll * E + 4); }
+
+template <typename T>
+cudaError_t balance_launch(const Plan& p, const void* logits, long long ld, const int* idx, int T_rows, int E, int k, int act, const int* seg,
+                           int n_seg, float* part_p, int* part_c, int* part_n, cudaStream_t s) {
+  const int vec = (((uintptr_t)logits | (uintptr_t)(ld * (long long)sizeof(T))) & 15u) == 0;
+#define MIX_BALANCE(G, V)                                                                                                                 \
+  return p.warps == 1 ? launch_pdl(kPdlHook, balance_kernel<T, G, V, 1>, dim3(p.units), dim3(32), 0, s, static_cast<const T*>(logits), ld, vec, \
+                                   idx, T_rows, E, k, act, seg, n_seg, p.unit_rows, part_p, part_c, part_n)                                     \
+                      : launch_pdl(kPdlHook, balance_kernel<T, G, V, kUnitWarps>, dim3(p.units), dim3(32 * kUnitWarps), 0, s,                    \
+                                   static_cast<const T*>(logits), ld, vec, idx, T_rows, E, k, act, seg, n_seg, p.unit_rows, part_p, part_c, part_n)
+  MIX_ROW_LAYOUT(E, MIX_BALANCE);
+#undef MIX_BALANCE
+}
+template <typename T>
+cudaError_t grad_launch(const void* logits, long long ld, const int* idx, int T_rows, int E, int k, int act, const int* seg, int n_seg,
+                        const int* counts, const int* rows, const float* d_loss, void* d_logits, long long ld_d, cudaStream_t s) {
+  const int vec = (((uintptr_t)logits | (uintptr_t)(ld * (long long)sizeof(T))) & 15u) == 0;
+  const int vec_d = (((uintptr_t)d_logits | (uintptr_t)(ld_d * (long long)sizeof(T))) & 15u) == 0;
+  const int warp_rows = T_rows >= 32768 ? 16 : (T_rows >= 8192 ? 8 : 4);
+  const long long ctas = ((long long)T_rows + 8 * warp_rows - 1) / (8 * warp_rows);
+#define MIX_BALANCE_GRAD(G, V)                                                                                                          \
+  return launch_pdl(kPdlHook, balance_grad_kernel<T, G, V>, dim3((unsigned)ctas), dim3(256), 0, s, static_cast<const T*>(logits), ld, vec, \
+                    idx, T_rows, E, k, act, seg, n_seg, counts, rows, d_loss, warp_rows, static_cast<T*>(d_logits), ld_d, vec_d)
+  MIX_ROW_LAYOUT(E, MIX_BALANCE_GRAD);
+#undef MIX_BALANCE_GRAD
+}
+
+int segment_args(const int* seg, int n_seg, char* errbuf, int errbuf_len) {
+  if (n_seg < 1 || n_seg > MIX_BALANCE_MAX_SEGMENTS) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "n_seg %d outside [1, %d]", n_seg, MIX_BALANCE_MAX_SEGMENTS);
+  if (!seg && n_seg != 1) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "without offsets there is one segment, not %d", n_seg);
+  return MIX_OK;
+}
+
+}  // namespace
+
+namespace mix {
+int router_args(const void* logits, int dtype, long long ld, int T, int E, int k, int act, char* errbuf, int errbuf_len);
+}
+
+extern "C" long long mix_router_balance_workspace(int T, int n_experts, int n_seg) {
+  if (T < 0 || n_experts < 1 || n_experts > kOpMaxExperts || n_seg < 1 || n_seg > MIX_BALANCE_MAX_SEGMENTS) return MIX_ERR_OUT_OF_RANGE;
+  int dev, n_sms;
+  if (op_device(&dev, &n_sms) != cudaSuccess) {
+    cudaGetLastError();
+    return MIX_ERR_CUDA;
+  }
+  return workspace_bytes_of(plan(T, n_seg, n_sms), n_experts);
+}
+
+extern "C" int mix_router_balance(const void* logits, int dtype, long long ld, const int* idx, int T, int n_experts, int k, int act,
+                                  const int* seg, int n_seg, float* loss, int* counts, float* mean_p, int* rows, void* workspace,
+                                  long long workspace_bytes, void* stream, char* errbuf, int errbuf_len) {
+  int rc = router_args(logits, dtype, ld, T, n_experts, k, act, errbuf, errbuf_len);
+  if (rc == MIX_OK) rc = segment_args(seg, n_seg, errbuf, errbuf_len);
+  if (rc != MIX_OK) return rc;
+  if ((T > 0 && !idx) || !loss || !counts || !mean_p || !rows) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "idx, loss, counts, mean_p and rows are required");
+  if (!workspace || ((uintptr_t)workspace & 3u)) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "the workspace is NULL or not on 4 bytes");
+  int dev, n_sms;
+  MIX_OP_CUDA(op_device(&dev, &n_sms));
+  const Plan p = plan(T, n_seg, n_sms);
+  if (workspace_bytes < workspace_bytes_of(p, n_experts))
+    MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "the workspace has to hold %lld bytes", workspace_bytes_of(p, n_experts));
+  float* part_p = static_cast<float*>(workspace);
+  int* part_c = reinterpret_cast<int*>(part_p + p.slots * n_experts);
+  int* part_n = part_c + p.slots * n_experts;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (T > 0) {
+    cudaError_t e;
+    if (dtype == MIX_DTYPE_F32) e = balance_launch<float>(p, logits, ld, idx, T, n_experts, k, act, seg, n_seg, part_p, part_c, part_n, s);
+    else if (dtype == MIX_DTYPE_BF16) e = balance_launch<__nv_bfloat16>(p, logits, ld, idx, T, n_experts, k, act, seg, n_seg, part_p, part_c, part_n, s);
+    else e = balance_launch<__half>(p, logits, ld, idx, T, n_experts, k, act, seg, n_seg, part_p, part_c, part_n, s);
+    MIX_OP_CUDA(e);
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(n_seg * p.cluster));
+  cfg.blockDim = dim3(kFinThreads);
+  cfg.stream = s;
+  cudaLaunchAttribute at[2];
+  int n_at = 0;
+  if (p.cluster > 1) {
+    at[n_at].id = cudaLaunchAttributeClusterDimension;
+    at[n_at].val.clusterDim.x = p.cluster;
+    at[n_at].val.clusterDim.y = 1;
+    at[n_at++].val.clusterDim.z = 1;
+  }
+  if (pdl_mask() & kPdlHook) {
+    at[n_at].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[n_at++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  cfg.attrs = at;
+  cfg.numAttrs = n_at;
+  MIX_OP_CUDA(cudaLaunchKernelEx(&cfg, balance_finish_kernel, static_cast<const float*>(part_p), static_cast<const int*>(part_c),
+                                 static_cast<const int*>(part_n), T, n_experts, seg, p.unit_rows, p.cluster, loss, counts, mean_p, rows));
+  return MIX_OK;
+}
+
+extern "C" int mix_router_balance_grad(const void* logits, int dtype, long long ld, const int* idx, int T, int n_experts, int k, int act,
+                                       const int* seg, int n_seg, const int* counts, const int* rows, const float* d_loss, void* d_logits,
+                                       long long ld_d, void* stream, char* errbuf, int errbuf_len) {
+  int rc = router_args(logits, dtype, ld, T, n_experts, k, act, errbuf, errbuf_len);
+  if (rc == MIX_OK) rc = segment_args(seg, n_seg, errbuf, errbuf_len);
+  if (rc != MIX_OK) return rc;
+  if (ld_d < n_experts) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "row stride %lld of d_logits is below n_experts %d", ld_d, n_experts);
+  if (T == 0) return MIX_OK;
+  if (!idx || !counts || !rows || !d_loss || !d_logits) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "idx, counts, rows, d_loss and d_logits are required");
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  if (dtype == MIX_DTYPE_F32) e = grad_launch<float>(logits, ld, idx, T, n_experts, k, act, seg, n_seg, counts, rows, d_loss, d_logits, ld_d, s);
+  else if (dtype == MIX_DTYPE_BF16) e = grad_launch<__nv_bfloat16>(logits, ld, idx, T, n_experts, k, act, seg, n_seg, counts, rows, d_loss, d_logits, ld_d, s);
+  else e = grad_launch<__half>(logits, ld, idx, T, n_experts, k, act, seg, n_seg, counts, rows, d_loss, d_logits, ld_d, s);
+  MIX_OP_CUDA(e);
+  return MIX_OK;
+}
