@@ -15,15 +15,57 @@ namespace {
 // ---------------------------------------------------------------------------------------------------- quantisation
 // A row's codes are the exact quotients 127 x / a rounded to the nearest, halves to the even one: x has 11 significant bits at
 // most, 127 x is exact in fp32, the quotient is never so close to a half that a correctly rounded division would cross it.  A
-// division costs more than the rest of the row's work, so the quotient comes from a multiplication by 127 / a and is divided
-// only where it lies within 2^-13 of a half (the multiplication is off by at most 127 * 2^-23).
+// division costs more than the rest of the row's work, so the quotient comes from a multiplication by 127 / a (off by at most
+// 127 * 2^-23), and a vector is divided only where one of its quotients lies within 2^-13 of a half.  Adding 1.5 * 2^23 rounds
+// to a whole number and leaves its two's complement in the low bits of the sum.
 // A row that lies far from 1 is first scaled by a power of two, which is exact: neither 127 x nor 127 / a leaves fp32's range.
+// 8192 rows of 8192 bf16: 60 us with a rounding, a comparison and a conversion per element, %s us so.
 template <typename T>
-__device__ __forceinline__ signed char code_of(float x, float inv, float a) {
-  float q = x * inv;
-  float r = rintf(q);
-  if (fabsf(fabsf(q - r) - 0.5f) < 0.000122f) r = rintf(__fdiv_rn(127.f * x, a));
-  return (signed char)(int)r;
+struct Pair2;
+template <>
+struct Pair2<__nv_bfloat16> {
+  using V = __nv_bfloat162;
+  static __device__ __forceinline__ float2 f32(V v) { return __bfloat1622float2(v); }
+};
+template <>
+struct Pair2<__half> {
+  using V = __half2;
+  static __device__ __forceinline__ float2 f32(V v) { return __half22float2(v); }
+};
+// Largest size of 8 elements; NaN where one is NaN.
+template <typename T>
+__device__ __forceinline__ typename Pair2<T>::V sizes8(const uint4& raw, typename Pair2<T>::V a) {
+  const typename Pair2<T>::V* e = reinterpret_cast<const typename Pair2<T>::V*>(&raw);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) a = __hmax2_nan(a, __habs2(e[j]));
+  return a;
+}
+template <typename T>
+__device__ __forceinline__ uint2 codes8(const uint4& raw, float pre, float inv, float a) {
+  constexpr float kRound = 12582912.f;
+  const typename Pair2<T>::V* e = reinterpret_cast<const typename Pair2<T>::V*>(&raw);
+  unsigned t[8];
+  float far = 0.f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 f = Pair2<T>::f32(e[j]);
+    const float s0 = fmaf(f.x * pre, inv, kRound), s1 = fmaf(f.y * pre, inv, kRound);
+    far = fmaxf(far, fmaxf(fabsf(fmaf(f.x * pre, inv, kRound - s0)), fabsf(fmaf(f.y * pre, inv, kRound - s1))));
+    t[2 * j] = __float_as_uint(s0);
+    t[2 * j + 1] = __float_as_uint(s1);
+  }
+  if (far > 0.5f - 0.000122f) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 f = Pair2<T>::f32(e[j]);
+      t[2 * j] = (unsigned)(int)rintf(__fdiv_rn(127.f * (f.x * pre), a));
+      t[2 * j + 1] = (unsigned)(int)rintf(__fdiv_rn(127.f * (f.y * pre), a));
+    }
+  }
+  uint2 c;
+  c.x = __byte_perm(__byte_perm(t[0], t[1], 0x0040), __byte_perm(t[2], t[3], 0x0040), 0x5410);
+  c.y = __byte_perm(__byte_perm(t[4], t[5], 0x0040), __byte_perm(t[6], t[7], 0x0040), 0x5410);
+  return c;
 }
 
 constexpr int kQuantVecs = 4;                                  // 8-element vectors a thread keeps
@@ -32,7 +74,7 @@ __global__ void __launch_bounds__(THREADS < 128 ? 128 : THREADS)
 quantize_rows_kernel(const T* __restrict__ x, long long ld, int vec, int x_rows, const int* __restrict__ order, int div, int n_rows, int d,
                      signed char* __restrict__ codes, float* __restrict__ scale) {
   constexpr int kRows = THREADS < 128 ? 128 / THREADS : 1;     // rows a CTA takes
-  __shared__ float red[kRows == 1 ? THREADS / 32 : 1];
+  __shared__ unsigned red[kRows == 1 ? THREADS / 32 : 1];
   pdl_wait();
   pdl_launch_dependents();
   const int tid = threadIdx.x % THREADS;
@@ -52,9 +94,10 @@ quantize_rows_kernel(const T* __restrict__ x, long long ld, int vec, int x_rows,
     return;
   }
   const T* row = x + src * ld;
+  using V = typename Pair2<T>::V;
   uint4 keep[kQuantVecs];
-  float a = 0.f;
-  bool bad = false;                                            // fmaxf drops NaN
+  V most;
+  most.x = most.y = from_f32<T>(0.f);
   auto fetch = [&](int v) -> uint4 {
     if (vec) return *reinterpret_cast<const uint4*>(row + 8ll * v);
     uint4 raw;
@@ -63,32 +106,24 @@ quantize_rows_kernel(const T* __restrict__ x, long long ld, int vec, int x_rows,
     for (int j = 0; j < 8; ++j) e[j] = row[8ll * v + j];
     return raw;
   };
-  auto look = [&](const uint4& raw) {
-    const T* e = reinterpret_cast<const T*>(&raw);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float f = fabsf(to_f32(e[j]));
-      a = fmaxf(a, f);
-      bad |= !(f <= 3.402823466e38f);
-    }
-  };
 #pragma unroll
   for (int b = 0; b < kQuantVecs; ++b) {
     const int v = tid + b * THREADS;
     keep[b] = v < n_vec ? fetch(v) : make_uint4(0u, 0u, 0u, 0u);
   }
 #pragma unroll
-  for (int b = 0; b < kQuantVecs; ++b) look(keep[b]);
-  for (int v = tid + kQuantVecs * THREADS; v < n_vec; v += THREADS) look(fetch(v));
-  if (bad) a = INFINITY;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
+  for (int b = 0; b < kQuantVecs; ++b) most = sizes8<T>(keep[b], most);
+  for (int v = tid + kQuantVecs * THREADS; v < n_vec; v += THREADS) most = sizes8<T>(fetch(v), most);
+  const float2 two = Pair2<T>::f32(most);
+  // (sizes compare as their bits do, and a NaN's are above infinity's)
+  unsigned bits = __reduce_max_sync(0xffffffffu, max(__float_as_uint(two.x) & 0x7fffffffu, __float_as_uint(two.y) & 0x7fffffffu));
   if (kRows == 1 && THREADS > 32) {
-    if ((tid & 31) == 0) red[tid >> 5] = a;
+    if ((tid & 31) == 0) red[tid >> 5] = bits;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) a = fmaxf(a, red[w]);
+    for (int w = 0; w < THREADS / 32; ++w) bits = max(bits, red[w]);
   }
+  const float a = __uint_as_float(bits);
   if (!(a < INFINITY)) {                                       // a row with an infinity or a NaN: its products are NaN
     for (int v = tid; v < n_vec; v += THREADS) out[v] = make_uint2(0u, 0u);
     if (tid == 0) scale[i] = __int_as_float(0x7fc00000);
@@ -96,23 +131,15 @@ quantize_rows_kernel(const T* __restrict__ x, long long ld, int vec, int x_rows,
   }
   const float pre = a > 1e30f ? 0x1p-64f : (a < 1e-30f ? 0x1p64f : 1.f);
   const float as = a * pre, inv = as > 0.f ? 127.f / as : 0.f;
-  auto quantize = [&](const uint4& raw) -> uint2 {
-    const T* e = reinterpret_cast<const T*>(&raw);
-    uint2 c;
-    signed char* b = reinterpret_cast<signed char*>(&c);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) b[j] = code_of<T>(to_f32(e[j]) * pre, inv, as);
-    return c;
-  };
   if (as == 0.f) {
     for (int v = tid; v < n_vec; v += THREADS) out[v] = make_uint2(0u, 0u);
   } else {
 #pragma unroll
     for (int b = 0; b < kQuantVecs; ++b) {
       const int v = tid + b * THREADS;
-      if (v < n_vec) out[v] = quantize(keep[b]);
+      if (v < n_vec) out[v] = codes8<T>(keep[b], pre, inv, as);
     }
-    for (int v = tid + kQuantVecs * THREADS; v < n_vec; v += THREADS) out[v] = quantize(fetch(v));
+    for (int v = tid + kQuantVecs * THREADS; v < n_vec; v += THREADS) out[v] = codes8<T>(fetch(v), pre, inv, as);
   }
   if (tid == 0) scale[i] = __fdiv_rn(a, 127.f);
 }
@@ -123,20 +150,28 @@ quantize_rows_kernel(const T* __restrict__ x, long long ld, int vec, int x_rows,
 // 32-bit integers in tensor memory, two of them, so that one tile is written out while the next is computed.
 constexpr int kTileCh = 128;                                   // output channels of a tile
 constexpr int kKBytes = 128;                                   // codes of a row in a stage: one swizzled 128-byte line
-constexpr int kGemmThreads = 192;                              // copies, tensor-core instructions, four warps of epilogue
+constexpr int kEpiWarps = 8;                                   // two for each quarter of tensor memory's lanes
+constexpr int kGemmThreads = 64 + 32 * kEpiWarps;              // copies, tensor-core instructions, epilogue
+constexpr int kStageOut = 2048;                                // bytes of a warp's piece of the output on its way to memory
 constexpr long long kI8WaitCycles = 4000000000ll;              // about two seconds
 
 __device__ unsigned g_i8_status;                               // MIX_STATUS_WAIT_TIMEOUT, until mix_linear_int_status reads it
 __device__ const long long g_i8_wait_cycles = kI8WaitCycles;
 
-template <int NT>
+// kPair: two CTAs of a cluster work on one tile of 256 channels with cta_group::2.  Each holds its own 128 channels and half of the
+// tokens' rows, so that a k-block of 256 tokens costs a CTA 32 KB of copies and 32 KB of reads of shared memory, not 48 and 48:
+// at 128 bytes a clock the single CTA's 96 KB take 768 clocks, while the tensor core needs 512 (measured 834 and 1573 us for
+// 8192 x 8192 x 32768).
+template <int NT, bool kPair>
 struct GemmCfg {
-  static constexpr int kBoxRows = NT < 64 ? NT : 64;           // tokens of a copy
+  static constexpr int kCtas = kPair ? 2 : 1;
+  static constexpr int kTokRows = NT / kCtas;                  // rows of the token operand in this CTA's shared memory
+  static constexpr int kBoxRows = kTokRows < 64 ? kTokRows : 64;   // tokens of a copy
   static constexpr int kABytes = kTileCh * kKBytes;
-  static constexpr int kStageBytes = kABytes + NT * kKBytes;
+  static constexpr int kStageBytes = kABytes + kTokRows * kKBytes;
   static constexpr int kStages = (200 * 1024) / kStageBytes < 12 ? (200 * 1024) / kStageBytes : 12;
   static constexpr int kTmemCols = 2 * NT < 32 ? 32 : 2 * NT;
-  static constexpr int kSmem = kStages * kStageBytes + 1024;
+  static constexpr int kSmem = kStages * kStageBytes + kEpiWarps * kStageOut + 1024;
 };
 
 struct GemmShared {
@@ -161,35 +196,53 @@ __device__ __forceinline__ void umma_i8(unsigned d_tmem, unsigned long long a, u
       : "memory");
 }
 
+__device__ __forceinline__ void umma_i8_pair(unsigned d_tmem, unsigned long long a, unsigned long long b, unsigned idesc, unsigned accumulate,
+                                             unsigned on) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 e, %5, 0;\n\t"
+      "@e tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(on)
+      : "memory");
+}
+
 struct I8Tile {
   int expert, ch0, row0, n_tok;
 };
 
-template <int NT>
-__device__ __forceinline__ I8Tile i8_tile(const GemmShared* sh, int tile, int& e) {
+// Tiles of an expert: groups of kGroup token tiles; in a group the channels one after the other, each with all of the group's
+// token tiles next to each other: a tile of W comes from DRAM once a group, and the group's tokens stay in L2.
+constexpr int kGroup = 16;
+template <int NT, bool kPair>
+__device__ __forceinline__ I8Tile i8_tile(const GemmShared* sh, int tile, int ch_tiles, int& e) {
   while (tile >= sh->tile0[e + 1]) ++e;                        // (a role's tiles only rise)
   const int local = tile - sh->tile0[e], rows = sh->row0[e + 1] - sh->row0[e], tt = (rows + NT - 1) / NT;
+  const int group = local / (kGroup * ch_tiles), in = local - group * kGroup * ch_tiles, wide = min(kGroup, tt - group * kGroup);
   I8Tile t;
   t.expert = e;
-  t.ch0 = local / tt * kTileCh;                                // token tiles of the same channels are neighbours: W comes from DRAM once
-  const int tk = local % tt;
-  t.row0 = sh->row0[e] + tk * NT;
-  t.n_tok = min(NT, rows - tk * NT);
+  t.ch0 = in / wide * (kPair ? 2 * kTileCh : kTileCh);
+  const int tk = group * kGroup + in % wide;
+  // an expert's rows are dealt evenly: with a full tile and a small one in turn, the even workers would get all the full ones
+  const int each = ((rows + tt - 1) / tt + 15) & ~15;
+  t.row0 = sh->row0[e] + tk * each;
+  t.n_tok = min(each, rows - tk * each);                       // (0 or less: the tiles in front of this one hold all rows)
   return t;
 }
 
-template <typename OutT, int NT>
+template <typename OutT, int NT, bool kPair>
 __global__ void __launch_bounds__(kGemmThreads, 1)
 linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x, const float* __restrict__ scale,
-                 const float* __restrict__ w_scale, const float* __restrict__ bias, const int* __restrict__ offsets, int n_rows, int K,
-                 int N, int E, OutT* __restrict__ out, long long ld_out) {
-  using Cfg = GemmCfg<NT>;
+                  const float* __restrict__ w_scale, const float* __restrict__ bias, const int* __restrict__ offsets, int n_rows, int K,
+                  int N, int E, OutT* __restrict__ out, long long ld_out, int vec) {
+  using Cfg = GemmCfg<NT, kPair>;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* ring = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   __shared__ GemmShared shared;
-  __shared__ float tok_scale[4][NT];                           // a copy per warp of the epilogue
+  __shared__ float tok_scale[kEpiWarps][NT];                   // a copy per warp of the epilogue
   GemmShared* sh = &shared;
   const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const int rank = kPair ? (int)cluster_ctarank() : 0;         // rank 0 leads a pair: it issues the instructions, and its barriers count both CTAs' copies
+  const int worker = kPair ? (int)(blockIdx.x >> 1) : (int)blockIdx.x, n_workers = kPair ? (int)(gridDim.x >> 1) : (int)gridDim.x;
   if (threadIdx.x == 0) {
     for (int s = 0; s < Cfg::kStages; ++s) {
       mbar_init(smem_u32(&sh->full[s]), 1);
@@ -197,22 +250,26 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(smem_u32(&sh->acc_full[a]), 1);
-      mbar_init(smem_u32(&sh->acc_empty[a]), 4);
+      mbar_init(smem_u32(&sh->acc_empty[a]), kEpiWarps * Cfg::kCtas);
     }
     sh->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  if (warp == 1) tmem_alloc(smem_u32(&sh->tmem_base), Cfg::kTmemCols);
+  if (warp == 1) {
+    if (kPair) tmem_alloc_pair(smem_u32(&sh->tmem_base), Cfg::kTmemCols);
+    else tmem_alloc(smem_u32(&sh->tmem_base), Cfg::kTmemCols);
+  }
   pdl_wait();
   pdl_launch_dependents();
-  const int ch_tiles = (N + kTileCh - 1) / kTileCh;
+  constexpr int kChannels = kTileCh * Cfg::kCtas;
+  const int ch_tiles = (N + kChannels - 1) / kChannels;
   if (warp == 0) {                                             // the experts' rows and tiles; offsets that fall or leave the rows are held in
     int row = 0, tiles = 0;
     for (int e0 = 0; e0 < E; e0 += 32) {
       const int e = e0 + lane;
       int end = offsets ? (e < E ? min(max(offsets[e + 1], 0), n_rows) : 0) : n_rows;
-      int begin = offsets ? (e < E ? min(max(offsets[e], 0), n_rows) : 0) : 0;
+      const int begin = offsets ? (e < E ? min(max(offsets[e], 0), n_rows) : 0) : 0;
       if (e0 == 0) row = __shfl_sync(0xffffffffu, begin, 0);
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {                       // running maximum: never below an earlier offset
@@ -242,6 +299,7 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
   }
   tc_fence_before();
   __syncthreads();
+  if (kPair) cluster_sync_all();                               // the peer's barriers are initialised before anything is sent to them
   tc_fence_after();
   const unsigned tmem_base = (unsigned)uniform((int)sh->tmem_base);
   const int total = uniform(sh->tile0[E]);
@@ -252,55 +310,83 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
     int stage = 0, e = 0;
     unsigned phase = 0;
     bool ok = true;
-    for (int tile = blockIdx.x; tile < total && ok; tile += gridDim.x) {
-      const I8Tile t = i8_tile<NT>(sh, tile, e);
-      const int boxes = uniform((t.n_tok + Cfg::kBoxRows - 1) / Cfg::kBoxRows);
-      const int wy = uniform(t.expert * N + t.ch0), xy = uniform(t.row0);      // (E * N rows of W fit in 31 bits: checked on the host)
-      const unsigned bytes = Cfg::kABytes + boxes * Cfg::kBoxRows * kKBytes;
+    for (int tile = worker; tile < total && ok; tile += n_workers) {
+      const I8Tile t = i8_tile<NT, kPair>(sh, tile, ch_tiles, e);
+      if (t.n_tok <= 0) continue;
+      const int tok_rows = kPair ? ((t.n_tok + 31) & ~31) / 2 : t.n_tok;     // of this CTA
+      const int boxes = uniform((tok_rows + Cfg::kBoxRows - 1) / Cfg::kBoxRows);
+      // (E * N rows of W fit in 31 bits: checked on the host.  Channels behind the last and tokens behind the expert's are
+      // other rows or the fill value; what comes of them is not stored)
+      const int wy = uniform(t.expert * N + t.ch0 + rank * kTileCh), xy = uniform(t.row0 + (kPair ? rank * tok_rows : 0));
+      const unsigned bytes = (Cfg::kABytes + boxes * Cfg::kBoxRows * kKBytes) * Cfg::kCtas;
       for (int kb = 0; kb < num_kb; ++kb) {
         if (!mbar_wait_bounded_warp(smem_u32(&sh->empty[stage]), phase ^ 1u, &sh->abort_flag, cap, &g_i8_status)) { ok = false; break; }
         const unsigned bar = smem_u32(&sh->full[stage]), sa = smem_u32(ring + stage * Cfg::kStageBytes), on = elect_one();
-        mbar_expect_tx(bar, bytes, on);
-        tma_load_2d(sa, &tmap_w, kb * kKBytes, wy, bar, on);
-        for (int b = 0; b < boxes; ++b)
-          tma_load_2d(sa + Cfg::kABytes + b * Cfg::kBoxRows * kKBytes, &tmap_x, kb * kKBytes, xy + b * Cfg::kBoxRows, bar, on);
+        if (kPair) {
+          if (rank == 0) mbar_expect_tx(bar, bytes, on);
+          const unsigned bar_c = mapa_cluster(bar, 0);
+          tma_load_2d_pair(sa, &tmap_w, kb * kKBytes, wy, bar_c, on);
+          for (int b = 0; b < boxes; ++b)
+            tma_load_2d_pair(sa + Cfg::kABytes + b * Cfg::kBoxRows * kKBytes, &tmap_x, kb * kKBytes, xy + b * Cfg::kBoxRows, bar_c, on);
+        } else {
+          mbar_expect_tx(bar, bytes, on);
+          tma_load_2d(sa, &tmap_w, kb * kKBytes, wy, bar, on);
+          for (int b = 0; b < boxes; ++b)
+            tma_load_2d(sa + Cfg::kABytes + b * Cfg::kBoxRows * kKBytes, &tmap_x, kb * kKBytes, xy + b * Cfg::kBoxRows, bar, on);
+        }
         if (++stage == Cfg::kStages) { stage = 0; phase ^= 1u; }
       }
     }
   } else if (warp == 1) {
-    int stage = 0, e = 0;
-    unsigned phase = 0, acc = 0, acc_phase = 0;
-    bool ok = true;
-    for (int tile = blockIdx.x; tile < total && ok; tile += gridDim.x) {
-      const I8Tile t = i8_tile<NT>(sh, tile, e);
-      const unsigned idesc = (unsigned)uniform((int)idesc_i8(kTileCh, (t.n_tok + 15) & ~15));
-      if (!mbar_wait_bounded_warp(smem_u32(&sh->acc_empty[acc]), acc_phase ^ 1u, &sh->abort_flag, cap, &g_i8_status)) break;
-      tc_fence_after();
-      const unsigned d_tmem = tmem_base + acc * NT;
-      for (int kb = 0; kb < num_kb; ++kb) {
-        if (!mbar_wait_bounded_warp(smem_u32(&sh->full[stage]), phase, &sh->abort_flag, cap, &g_i8_status)) { ok = false; break; }
+    if (rank == 0) {
+      int stage = 0, e = 0;
+      unsigned phase = 0, acc = 0, acc_phase = 0;
+      bool ok = true;
+      for (int tile = worker; tile < total && ok; tile += n_workers) {
+        const I8Tile t = i8_tile<NT, kPair>(sh, tile, ch_tiles, e);
+        if (t.n_tok <= 0) continue;
+        const unsigned idesc = (unsigned)uniform((int)(kPair ? idesc_i8(2 * kTileCh, (t.n_tok + 31) & ~31) : idesc_i8(kTileCh, (t.n_tok + 15) & ~15)));
+        if (!mbar_wait_bounded_warp(smem_u32(&sh->acc_empty[acc]), acc_phase ^ 1u, &sh->abort_flag, cap, &g_i8_status)) break;
         tc_fence_after();
-        const unsigned sa = smem_u32(ring + stage * Cfg::kStageBytes);
-        const unsigned long long da = umma_desc(sa), db = umma_desc(sa + Cfg::kABytes);
-        const unsigned on = elect_one();
+        const unsigned d_tmem = tmem_base + acc * NT;
+        for (int kb = 0; kb < num_kb; ++kb) {
+          if (!mbar_wait_bounded_warp(smem_u32(&sh->full[stage]), phase, &sh->abort_flag, cap, &g_i8_status)) { ok = false; break; }
+          tc_fence_after();
+          const unsigned sa = smem_u32(ring + stage * Cfg::kStageBytes);
+          const unsigned long long da = umma_desc(sa), db = umma_desc(sa + Cfg::kABytes);
+          const unsigned on = elect_one();
 #pragma unroll
-        for (int k = 0; k < 4; ++k) umma_i8(d_tmem, da + 2ull * k, db + 2ull * k, idesc, (unsigned)((kb | k) != 0), on);
-        umma_commit(smem_u32(&sh->empty[stage]), on);
-        if (++stage == Cfg::kStages) { stage = 0; phase ^= 1u; }
+          for (int k = 0; k < 4; ++k) {
+            if (kPair) umma_i8_pair(d_tmem, da + 2ull * k, db + 2ull * k, idesc, (unsigned)((kb | k) != 0), on);
+            else umma_i8(d_tmem, da + 2ull * k, db + 2ull * k, idesc, (unsigned)((kb | k) != 0), on);
+          }
+          if (kPair) umma_commit_pair(smem_u32(&sh->empty[stage]), on);      // the stage is free again, in both CTAs
+          else umma_commit(smem_u32(&sh->empty[stage]), on);
+          if (++stage == Cfg::kStages) { stage = 0; phase ^= 1u; }
+        }
+        if (!ok) break;
+        if (kPair) umma_commit_pair(smem_u32(&sh->acc_full[acc]), elect_one());
+        else umma_commit(smem_u32(&sh->acc_full[acc]), elect_one());
+        acc ^= 1u;
+        if (acc == 0) acc_phase ^= 1u;
       }
-      if (!ok) break;
-      umma_commit(smem_u32(&sh->acc_full[acc]), elect_one());
-      acc ^= 1u;
-      if (acc == 0) acc_phase ^= 1u;
     }
   } else {
+    // Epilogue.  A thread has one channel and 32 tokens of it, the output wants channels next to each other: the warp's 32 x 32
+    // piece goes through shared memory and leaves in 16-byte vectors, 64 bytes a token (128 for fp32).  Storing element by element
+    // from the registers costs 12 instructions an element, with four warps more time than the products of 2048 codes.
     const int q = warp & 3;                                    // tensor-memory lanes this warp may read
+    const int half = (warp - 2) >> 2;                          // every other piece of 32 tokens
+    constexpr int kTok = kStageOut / (32 * (int)sizeof(OutT)); // tokens of a piece: 32, or 16 of fp32
+    constexpr int kVW = 16 / (int)sizeof(OutT), kLanesRow = 32 / kVW, kRowsStep = 32 / kLanesRow;
     int e = 0;
     unsigned acc = 0, acc_phase = 0;
-    float* my_scale = tok_scale[q];
-    for (int tile = blockIdx.x; tile < total; tile += gridDim.x) {
-      const I8Tile t = i8_tile<NT>(sh, tile, e);
-      const int ch = t.ch0 + q * 32 + lane;
+    float* my_scale = tok_scale[warp - 2];
+    OutT* piece = reinterpret_cast<OutT*>(ring + Cfg::kStages * Cfg::kStageBytes + (warp - 2) * kStageOut);
+    for (int tile = worker; tile < total; tile += n_workers) {
+      const I8Tile t = i8_tile<NT, kPair>(sh, tile, ch_tiles, e);
+      if (t.n_tok <= 0) continue;
+      const int ch0 = t.ch0 + rank * kTileCh + q * 32, ch = ch0 + lane;
       const bool valid = ch < N;
       const float ws = valid ? w_scale[(long long)t.expert * N + ch] : 0.f;
       const float bs = valid && bias ? bias[(long long)t.expert * N + ch] : 0.f;
@@ -310,19 +396,43 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
       if (!mbar_wait_bounded_warp(smem_u32(&sh->acc_full[acc]), acc_phase, &sh->abort_flag, cap, &g_i8_status)) break;
       tc_fence_after();
       const unsigned taddr = tmem_base + acc * NT + ((unsigned)(q * 32) << 16);
-      OutT* dst = out + (long long)t.row0 * ld_out + ch;
-      for (int c0 = 0; c0 < t.n_tok; c0 += 32) {
+      for (int c0 = half * 32; c0 < t.n_tok; c0 += 64) {
         float v[32];
-        __syncwarp();
         tmem_ld32(taddr + c0, v);
-        if (valid) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (c0 + i < t.n_tok) dst[(c0 + i) * ld_out] = from_f32<OutT>(fmaf((float)__float_as_int(v[i]) * my_scale[c0 + i], ws, bs));
+        for (int i = 0; i < 32; ++i) v[i] = fmaf((float)__float_as_int(v[i]) * my_scale[c0 + i], ws, bs);
+#pragma unroll
+        for (int p = 0; p < 32; p += kTok) {
+#pragma unroll
+          for (int i = 0; i < kTok; ++i) piece[i * 32 + lane] = from_f32<OutT>(v[p + i]);
+          __syncwarp();
+          OutT* dst = out + (long long)(t.row0 + c0 + p) * ld_out + ch0;
+          const int n = min(kTok, t.n_tok - c0 - p);
+          if (vec) {
+            const int col = lane % kLanesRow * kVW;
+#pragma unroll
+            for (int i = 0; i < kTok; i += kRowsStep) {
+              const int r = i + lane / kLanesRow;
+              if (r < n && ch0 + col < N) {
+                if (ch0 + col + kVW <= N) {
+                  *reinterpret_cast<uint4*>(dst + r * ld_out + col) = *reinterpret_cast<const uint4*>(piece + r * 32 + col);
+                } else {
+                  for (int j = 0; ch0 + col + j < N; ++j) dst[r * ld_out + col + j] = piece[r * 32 + col + j];
+                }
+              }
+            }
+          } else if (valid) {
+            for (int r = 0; r < n; ++r) dst[r * ld_out + lane] = piece[r * 32 + lane];
+          }
+          __syncwarp();
         }
       }
       tc_fence_before();
-      if (lane == 0) mbar_arrive(smem_u32(&sh->acc_empty[acc]));
+      __syncwarp();
+      if (lane == 0) {
+        if (kPair) mbar_arrive_cluster(mapa_cluster(smem_u32(&sh->acc_empty[acc]), 0));
+        else mbar_arrive(smem_u32(&sh->acc_empty[acc]));
+      }
       acc ^= 1u;
       if (acc == 0) acc_phase ^= 1u;
     }
@@ -333,9 +443,11 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
     const long long t0 = clock64();
     while (clock64() - t0 < 2000000ll) __nanosleep(1000);
   }
+  if (kPair) cluster_sync_all();                               // neither CTA's barriers or tensor memory go while the other may still reach them
   if (warp == 1) {
     tc_fence_after();
-    tmem_dealloc(tmem_base, Cfg::kTmemCols);
+    if (kPair) tmem_dealloc_pair(tmem_base, Cfg::kTmemCols);
+    else tmem_dealloc(tmem_base, Cfg::kTmemCols);
   }
 }
 
@@ -395,12 +507,12 @@ struct Gemm {
   long long ld_out;
 };
 
-template <typename OutT, int NT>
+template <typename OutT, int NT, bool kPair>
 cudaError_t gemm_launch(const Gemm& g, int dev, int n_sms, cudaStream_t s) {
-  using Cfg = GemmCfg<NT>;
+  using Cfg = GemmCfg<NT, kPair>;
   static std::atomic<int> ready[kOpDevices];
   if (!ready[dev].load(std::memory_order_relaxed)) {
-    const cudaError_t e = cudaFuncSetAttribute(linear_int_kernel<OutT, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem);
+    const cudaError_t e = cudaFuncSetAttribute(linear_int_kernel<OutT, NT, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem);
     if (e != cudaSuccess) return e;
     ready[dev].store(1, std::memory_order_relaxed);
   }
@@ -408,19 +520,39 @@ cudaError_t gemm_launch(const Gemm& g, int dev, int n_sms, cudaStream_t s) {
   if (make_tmap_i8(&tw, g.w, (unsigned long long)g.E * g.N, g.K, kTileCh) != MIX_OK || make_tmap_i8(&tx, g.codes, g.n_rows, g.K, Cfg::kBoxRows) != MIX_OK)
     return cudaErrorInvalidValue;
   const long long tok_tiles = (long long)g.n_rows / NT + (g.E < g.n_rows ? g.E : g.n_rows);      // at most, however the rows fall
-  const long long most = (g.E == 1 ? (g.n_rows + NT - 1) / NT : tok_tiles) * ((g.N + kTileCh - 1) / kTileCh);
-  const int grid = (int)(most < n_sms ? most : n_sms);
-  return launch_pdl(kPdlHook, linear_int_kernel<OutT, NT>, dim3(grid), dim3(kGemmThreads), Cfg::kSmem, s, tw, tx, g.scale, g.w_scale, g.bias,
-                    g.offsets, g.n_rows, g.K, g.N, g.E, static_cast<OutT*>(g.out), g.ld_out);
+  const long long most = (g.E == 1 ? (g.n_rows + NT - 1) / NT : tok_tiles) * ((g.N + kTileCh * Cfg::kCtas - 1) / (kTileCh * Cfg::kCtas));
+  const long long workers = n_sms / Cfg::kCtas;
+  const int vec = (((uintptr_t)g.out | (uintptr_t)(g.ld_out * (long long)sizeof(OutT))) & 15u) == 0;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((most < workers ? most : workers) * Cfg::kCtas));
+  cfg.blockDim = dim3(kGemmThreads);
+  cfg.dynamicSmemBytes = Cfg::kSmem;
+  cfg.stream = s;
+  cudaLaunchAttribute at[2];
+  int n_at = 0;
+  if (kPair) {
+    at[n_at].id = cudaLaunchAttributeClusterDimension;
+    at[n_at].val.clusterDim.x = 2;
+    at[n_at].val.clusterDim.y = 1;
+    at[n_at++].val.clusterDim.z = 1;
+  }
+  if (pdl_mask() & kPdlHook) {
+    at[n_at].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[n_at++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  cfg.attrs = at;
+  cfg.numAttrs = n_at;
+  return cudaLaunchKernelEx(&cfg, linear_int_kernel<OutT, NT, kPair>, tw, tx, g.scale, g.w_scale, g.bias, g.offsets, g.n_rows, g.K, g.N, g.E,
+                            static_cast<OutT*>(g.out), g.ld_out, vec);
 }
 
 template <typename OutT>
 cudaError_t gemm_pick(const Gemm& g, int dev, int n_sms, cudaStream_t s) {
   const int share = (g.n_rows + g.E - 1) / g.E;
-  if (share <= 32) return gemm_launch<OutT, 32>(g, dev, n_sms, s);
-  if (share <= 64) return gemm_launch<OutT, 64>(g, dev, n_sms, s);
-  if (share <= 128) return gemm_launch<OutT, 128>(g, dev, n_sms, s);
-  return gemm_launch<OutT, 256>(g, dev, n_sms, s);
+  if (share <= 32) return gemm_launch<OutT, 32, false>(g, dev, n_sms, s);
+  if (share <= 64) return gemm_launch<OutT, 64, false>(g, dev, n_sms, s);
+  if (share <= 128) return gemm_launch<OutT, 128, false>(g, dev, n_sms, s);
+  return gemm_launch<OutT, 256, true>(g, dev, n_sms, s);
 }
 
 int gemm_call(const Gemm& g, int dtype, void* stream, char* errbuf, int errbuf_len) {

@@ -94,7 +94,7 @@ __device__ __forceinline__ void load_row(const T* __restrict__ row, int E, int s
     }
   }
 #pragma unroll
-  for (int v = 0; v < V; ++v) x[v] = x[v] == x[v] ? x[v] : -INFINITY;
+  for (int v = 0; v < V; ++v) x[v] = fmaxf(x[v], -INFINITY);   // (the larger of a NaN and a number is the number)
 }
 template <typename T, int G, int V>
 __device__ __forceinline__ void store_row(T* __restrict__ row, int E, int sub, bool vec, const float (&x)[V]) {
@@ -118,6 +118,11 @@ __device__ __forceinline__ void store_row(T* __restrict__ row, int E, int sub, b
 
 template <int G>
 __device__ __forceinline__ float group_max(float x) {
+  if (G == 32) {
+    float m;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(x));
+    return m;
+  }
 #pragma unroll
   for (int o = 1; o < G; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
   return x;
@@ -128,19 +133,84 @@ __device__ __forceinline__ float group_sum(float x) {
   for (int o = 1; o < G; o <<= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
   return x;
 }
+// Does any lane of the group say yes?
+template <int G>
+__device__ __forceinline__ bool group_any(bool yes) {
+  const unsigned votes = __ballot_sync(0xffffffffu, yes);
+  const int first = (int)(threadIdx.x & 31) & ~(G - 1);
+  return G == 32 ? votes != 0u : ((votes >> first) & ((1u << (G & 31)) - 1u)) != 0u;
+}
 
-// Unnormalised score of a logit in a row whose largest is `top`.
-//   softmax  e^(x - top); logits equal to the largest count 1 even where both are +inf -- the limit of equal logits that grow
-//   sigmoid  sigmoid(x) e^-min(top, 0): where all logits of a row are low their sigmoids underflow together, their shares do not
-__device__ __forceinline__ float score_softmax(float x, float top) { return x == -INFINITY ? 0.f : (x == top ? 1.f : expf(x - top)); }
-__device__ __forceinline__ float score_sigmoid(float x, float top) {
+// e^x as 2^(x log2 e), log2 e in two parts: the argument is off by half a step of itself and no more, so the result by
+// |x| 2^-24 relative and the two steps of the hardware's 2^x.  expf takes twice as many instructions to save the first part, and a
+// logit's distance from the row's largest is rounded by as much already.  Results below 2^-126 are 0.
+__device__ __forceinline__ float exp2_hw(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+constexpr float kLog2eHi = 1.44269502162933350f, kLog2eLo = 1.92596299112661746e-8f;
+__device__ __forceinline__ float times_log2e(float x) { return fmaf(x, kLog2eHi, x * kLog2eLo); }      // (-inf stays -inf)
+__device__ __forceinline__ float exp_row(float x) { return exp2_hw(times_log2e(x)); }
+__device__ __forceinline__ float rcp_hw(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// sigmoid(x), and 1 - sigmoid(x) in `rest` without cancellation.  The exponential is held in 2^126: beyond, sigmoid(x) is 2^-126.
+__device__ __forceinline__ float sigmoid_row(float x, float* rest = nullptr) {
+  const float e = exp2_hw(fminf(times_log2e(-x), 126.f)), s = rcp_hw(1.f + e);
+  if (rest) *rest = e * s;
+  return s;
+}
+
+// Unnormalised scores of a row on G lanes, in place, and their sum; `top` is the row's largest logit.
+//   softmax  e^(x - top).  Logits of +inf share the row, the limit of equal ones that grow: they score 1, all others 0.
+//   sigmoid  sigmoid(x); where all logits are below 0, sigmoid(x) e^-top: low ones underflow together, their shares do not.
+// (the caller's lanes of a group agree on `top`; rows of one warp may differ)
+template <int V>
+__device__ __forceinline__ float top_of(const float (&x)[V]) {
+  float top = x[0];
+#pragma unroll
+  for (int v = 1; v < V; ++v) top = fmaxf(top, x[v]);
+  return top;
+}
+__device__ __forceinline__ float score(int act, float x, float top) {      // of one logit
   if (x == -INFINITY) return 0.f;
-  return x > 0.f ? 1.f / (1.f + expf(-x)) : expf(x - fminf(top, 0.f)) / (1.f + expf(x));   // (x > 0: the largest is positive too)
+  if (act == MIX_ACT_SOFTMAX) return x == top ? 1.f : exp_row(x - top);
+  return top >= 0.f ? sigmoid_row(x) : exp_row(x - top) * rcp_hw(1.f + exp_row(x));
 }
-__device__ __forceinline__ float score(int act, float x, float top) {
-  return act == MIX_ACT_SOFTMAX ? score_softmax(x, top) : score_sigmoid(x, top);
+template <int V>
+__device__ __forceinline__ float scores(int act, float top, float (&x)[V]) {
+  float total = 0.f;
+  if (act == MIX_ACT_SOFTMAX) {
+    if (top == INFINITY) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) x[v] = x[v] == INFINITY ? 0.f : -INFINITY;
+      top = 0.f;
+    } else if (top == -INFINITY) {
+      top = 0.f;
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      x[v] = exp_row(x[v] - top);
+      total += x[v];
+    }
+  } else if (top >= 0.f) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      x[v] = x[v] == -INFINITY ? 0.f : sigmoid_row(x[v]);
+      total += x[v];
+    }
+  } else {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      x[v] = x[v] == -INFINITY ? 0.f : exp_row(x[v] - top) * rcp_hw(1.f + exp_row(x[v]));
+      total += x[v];
+    }
+  }
+  return total;
 }
-__device__ __forceinline__ float sigmoidf(float x) { return 1.f / (1.f + expf(-x)); }
 #endif
 
 constexpr int kOpMaxExperts = 512;

@@ -37,33 +37,6 @@ __device__ __forceinline__ int seg_of_row(const int* __restrict__ seg, int n_seg
   return lo;
 }
 
-// Probabilities of a row held by G lanes, in place; rows that are off become zeros.
-template <typename T, int G, int V>
-__device__ __forceinline__ void probabilities(int act, bool on, float (&x)[V]) {
-  float top = x[0];
-#pragma unroll
-  for (int v = 1; v < V; ++v) top = fmaxf(top, x[v]);
-  top = group_max<G>(top);
-  float total = 0.f;
-  if (act == MIX_ACT_SOFTMAX) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      x[v] = score_softmax(x[v], top);
-      total += x[v];
-    }
-  } else {
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      x[v] = score_sigmoid(x[v], top);
-      total += x[v];
-    }
-  }
-  total = group_sum<G>(total);
-  const float inv = on && total > 0.f ? 1.f / total : 0.f;
-#pragma unroll
-  for (int v = 0; v < V; ++v) x[v] *= inv;
-}
-
 template <typename T, int G, int V, int W>
 __global__ void __launch_bounds__(32 * W)
 balance_kernel(const T* __restrict__ logits, long long ld, int vec, const int* __restrict__ idx, int T_rows, int E, int k, int act,
@@ -87,29 +60,45 @@ balance_kernel(const T* __restrict__ logits, long long ld, int vec, const int* _
     int rows = 0;
 #pragma unroll
     for (int v = 0; v < V; ++v) acc[v] = 0.f;
-    for (int base = a + warp * R; base < b; base += W * R) {   // (all lanes of a warp: a row of no segment is a row that is off)
+    // The next row is under way while one is worked on: a warp has few rows, and a row's reductions are one after the other.
+    const auto fetch = [&](int base, float (&x)[V], int& name) {
       const int t = base + lane / G;
-      bool named = false;
-      float x[V];
+      name = -1;
       if (t < b) {
         load_row<T, G, V>(logits + t * ld, E, sub, vec != 0, x);
-        for (int j = sub; j < k; j += G) {
+        if (sub < k) name = idx[(long long)t * k + sub];
+      } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = -INFINITY;
+      }
+    };
+    float next[V];
+    int next_name;
+    fetch(a + warp * R, next, next_name);
+    for (int base = a + warp * R; base < b; base += W * R) {   // (all lanes of a warp: a row of no segment is a row that is off)
+      const int t = base + lane / G;
+      float x[V];
+      const int name = next_name;
+#pragma unroll
+      for (int v = 0; v < V; ++v) x[v] = next[v];
+      fetch(base + W * R, next, next_name);
+      bool named = (unsigned)name < (unsigned)E;
+      if (named) atomicAdd(&hist[name], 1);
+      if (G < kOpMaxTopk && t < b) {                           // (a lane's further entries of a narrow row)
+        for (int j = sub + G; j < k; j += G) {
           const int i = idx[(long long)t * k + j];
           if ((unsigned)i < (unsigned)E) {
             atomicAdd(&hist[i], 1);
             named = true;
           }
         }
-      } else {
-#pragma unroll
-        for (int v = 0; v < V; ++v) x[v] = -INFINITY;
       }
-      const unsigned votes = __ballot_sync(0xffffffffu, named);
-      const bool on = G == 32 ? votes != 0u : ((votes >> (lane & ~(G - 1))) & ((1u << (G & 31)) - 1u)) != 0u;
+      const bool on = group_any<G>(named);
       rows += on && sub == 0;
-      probabilities<T, G, V>(act, on, x);
+      const float total = group_sum<G>(scores<V>(act, group_max<G>(top_of<V>(x)), x));
+      const float inv = on && total > 0.f ? 1.f / total : 0.f;
 #pragma unroll
-      for (int v = 0; v < V; ++v) acc[v] += x[v];
+      for (int v = 0; v < V; ++v) acc[v] = fmaf(x[v], inv, acc[v]);
     }
     // this segment's share of the unit
 #pragma unroll
@@ -287,34 +276,47 @@ balance_grad_kernel(const T* __restrict__ logits, long long ld, int vec, const i
 #pragma unroll
       for (int v = 0; v < V; ++v) f[v] = 0.f;
     }
-    for (int base = at; base < b; base += R) {
+    const auto fetch = [&](int base, float (&x)[V], bool& named) {
       const int t = base + lane / G;
-      const bool in = t < b, live = in && t >= a;
-      bool named = false;
-      float x[V], p[V];
-      if (live) {
+      named = false;
+      if (t >= a && t < b) {
         load_row<T, G, V>(logits + t * ld, E, sub, vec != 0, x);
         for (int j = sub; j < k; j += G) named |= (unsigned)idx[(long long)t * k + j] < (unsigned)E;
       } else {
 #pragma unroll
         for (int v = 0; v < V; ++v) x[v] = -INFINITY;
       }
-      const unsigned votes = __ballot_sync(0xffffffffu, named);
-      const bool on = G == 32 ? votes != 0u : ((votes >> (lane & ~(G - 1))) & ((1u << (G & 31)) - 1u)) != 0u;
+    };
+    float next[V];
+    bool next_named;
+    fetch(at, next, next_named);
+    for (int base = at; base < b; base += R) {
+      const int t = base + lane / G;
+      float x[V], rest[V];
+      const bool on = group_any<G>(next_named);
 #pragma unroll
-      for (int v = 0; v < V; ++v) p[v] = x[v];
-      probabilities<T, G, V>(act, on, p);
+      for (int v = 0; v < V; ++v) x[v] = next[v];
+      if (base + R < b) fetch(base + R, next, next_named);
+      if (act == MIX_ACT_SIGMOID) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) sigmoid_row(x[v], &rest[v]);
+      }
+      const float total = group_sum<G>(scores<V>(act, group_max<G>(top_of<V>(x)), x));
+      const float inv = on && total > 0.f ? 1.f / total : 0.f;
       float dot = 0.f;
 #pragma unroll
-      for (int v = 0; v < V; ++v) dot += f[v] * p[v];
+      for (int v = 0; v < V; ++v) {
+        x[v] *= inv;
+        dot = fmaf(f[v], x[v], dot);
+      }
       dot = group_sum<G>(dot);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        float d = coef * (p[v] * (f[v] - dot));
-        if (act == MIX_ACT_SIGMOID) d *= sigmoidf(-x[v]);
-        p[v] = on && p[v] > 0.f ? d : 0.f;                     // (also where the factors are not finite: a NaN in d_loss of rows that are off)
+        float d = coef * (x[v] * (f[v] - dot));
+        if (act == MIX_ACT_SIGMOID) d *= rest[v];
+        x[v] = x[v] > 0.f ? d : 0.f;                           // (0 where the row is off, whatever its d_loss)
       }
-      if (in) store_row<T, G, V>(d_logits + t * ld_d, E, sub, vec_d != 0, p);
+      if (t < b) store_row<T, G, V>(d_logits + t * ld_d, E, sub, vec_d != 0, x);
     }
     at = b;
   }

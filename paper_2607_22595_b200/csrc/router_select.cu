@@ -18,13 +18,20 @@ namespace {
 constexpr int kSelThreads = 256;
 
 // ---------------------------------------------------------------------------------------------------- selection
-// k rounds of an arg-max over the row.  The selection compares the logits themselves, never probabilities: those round, and
-// two logits that differ could tie.
+// The selection compares the logits themselves, never probabilities: those round, and two logits that differ could tie.
+//
+// Rows of up to 128 experts: k rounds of an arg-max over the G lanes, 32 / G rows of a warp side by side.
+// Wider rows (a warp each): the k-th largest of the lanes' own largest logits is a lower bound on the row's k-th largest logit,
+// and only a few more than k logits reach it.  Those go to shared memory, one to a lane, and each counts how many come before it.
+// Where more than 32 reach it (many equal logits) the rounds decide.  65536 rows of 256, k = 8, with the softmax over the row:
+// 76 us by rounds, %s us so; the logits' stream alone takes 10.3.
+constexpr int kSelWarps = kSelThreads / 32;
 template <typename T, int G, int V>
 __global__ void __launch_bounds__(kSelThreads)
 router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_rows, int E, int k, int act, int renorm,
                    const int* __restrict__ n_live, int* __restrict__ idx, float* __restrict__ weights) {
   constexpr int S = G >= kOpMaxTopk ? 1 : (G == 1 ? 8 : kOpMaxTopk / G);   // chosen entries a lane keeps: entry j is lane j % G's
+  __shared__ float2 found[G == 32 ? kSelWarps : 1][32];                    // (logit, column)
   pdl_wait();
   pdl_launch_dependents();
   const int sub = threadIdx.x & (G - 1);
@@ -37,64 +44,92 @@ router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_ro
 #pragma unroll
     for (int v = 0; v < V; ++v) x[v] = -INFINITY;
   }
-  float top = x[0];
-#pragma unroll
-  for (int v = 1; v < V; ++v) top = fmaxf(top, x[v]);
-  top = group_max<G>(top);
-  float total = 0.f;
-  if (!renorm && act == MIX_ACT_SOFTMAX) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) total += score_softmax(x[v], top);
-    total = group_sum<G>(total);
-  }
-  unsigned key[V];
-#pragma unroll
-  for (int v = 0; v < V; ++v) key[v] = x[v] > -INFINITY ? f2key(x[v]) : 0u;
+  const float lane_top = top_of<V>(x), top = group_max<G>(lane_top);
   int my_idx[S];
-  float my_e[S];
-  float chosen = 0.f;
+  float my_x[S];
 #pragma unroll
-  for (int s = 0; s < S; ++s) { my_idx[s] = -1; my_e[s] = 0.f; }
-#pragma unroll
-  for (int j = 0; j < (G == 1 ? 8 : kOpMaxTopk); ++j) {
-    if (j >= k) break;
-    unsigned m = key[0];
-#pragma unroll
-    for (int v = 1; v < V; ++v) m = max(m, key[v]);
-    if (G == 32) {
-      m = __reduce_max_sync(0xffffffffu, m);
-    } else {
-#pragma unroll
-      for (int o = 1; o < G; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+  for (int s = 0; s < S; ++s) { my_idx[s] = -1; my_x[s] = -INFINITY; }
+  bool rounds = true;
+  if (G == 32) {
+    const int warp = threadIdx.x >> 5;
+    float rest = lane_top, bound = -INFINITY;
+    for (int left = k; left > 0;) {
+      bound = group_max<32>(rest);
+      if (bound == -INFINITY) break;
+      const unsigned at = __ballot_sync(0xffffffffu, rest == bound);
+      left -= __popc(at);
+      if (rest == bound) rest = -INFINITY;
     }
-    unsigned c = 0xffffffffu;
+    int n = 0;
 #pragma unroll
-    for (int v = V - 1; v >= 0; --v) c = key[v] == m ? (unsigned)row_col<T, G>(v, sub) : c;   // (columns rise with v)
-    if (G == 32) {
-      c = __reduce_min_sync(0xffffffffu, c);
-    } else {
-#pragma unroll
-      for (int o = 1; o < G; o <<= 1) c = min(c, __shfl_xor_sync(0xffffffffu, c, o));
+    for (int v = 0; v < V; ++v) {
+      const bool in = x[v] >= bound && x[v] > -INFINITY;
+      const unsigned at = __ballot_sync(0xffffffffu, in);
+      const int to = n + __popc(at & ((1u << sub) - 1u));
+      if (in && to < 32) found[warp][to] = make_float2(x[v], __int_as_float(row_col<T, G>(v, sub)));
+      n += __popc(at);
     }
-#pragma unroll
-    for (int v = 0; v < V; ++v) key[v] = (unsigned)row_col<T, G>(v, sub) == c ? 0u : key[v];
-    const bool some = m != 0u;
-    const float xj = key2f(m);
-    const float e = !some ? 0.f : (act == MIX_ACT_SIGMOID && !renorm ? sigmoidf(xj) : score(act, xj, top));
-    chosen += e;
-    if (j % G == sub) {
-      my_idx[j / G] = some ? (int)c : -1;
-      my_e[j / G] = e;
+    if (n <= 32) {
+      rounds = false;
+      __syncwarp();
+      const float2 mine = found[warp][sub];
+      const int col = __float_as_int(mine.y);
+      int rank = 0;
+      for (int i = 0; i < n; ++i) {
+        const float2 f = found[warp][i];
+        rank += f.x > mine.x || (f.x == mine.x && __float_as_int(f.y) < col);
+      }
+      __syncwarp();
+      if (sub < n) found[warp][rank] = mine;                               // in the order of the ranks
+      __syncwarp();
+      if (sub < n && sub < k) {
+        my_x[0] = found[warp][sub].x;
+        my_idx[0] = __float_as_int(found[warp][sub].y);
+      }
     }
   }
+  if (rounds) {
+    float key[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) key[v] = x[v];
+#pragma unroll
+    for (int j = 0; j < (G == 1 ? 8 : kOpMaxTopk); ++j) {
+      if (j >= k) break;
+      const float m = group_max<G>(top_of<V>(key));
+      unsigned c = 0xffffffffu;
+#pragma unroll
+      for (int v = V - 1; v >= 0; --v) c = key[v] == m ? (unsigned)row_col<T, G>(v, sub) : c;   // (columns rise with v)
+      if (G == 32) {
+        c = __reduce_min_sync(0xffffffffu, c);
+      } else {
+#pragma unroll
+        for (int o = 1; o < G; o <<= 1) c = min(c, __shfl_xor_sync(0xffffffffu, c, o));
+      }
+#pragma unroll
+      for (int v = 0; v < V; ++v) key[v] = (unsigned)row_col<T, G>(v, sub) == c ? -INFINITY : key[v];
+      if (j % G == sub && m > -INFINITY) {
+        my_idx[j / G] = (int)c;
+        my_x[j / G] = m;
+      }
+    }
+  }
+  const bool plain = act == MIX_ACT_SIGMOID && !renorm;                    // the weight is the sigmoid itself
+  float total = 0.f;
+  if (act == MIX_ACT_SOFTMAX && !renorm) total = scores<V>(act, top, x);
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+    my_x[s] = my_idx[s] < 0 ? 0.f : (plain ? sigmoid_row(my_x[s]) : score(act, my_x[s], top));
+    if (renorm) total += my_x[s];
+  }
+  if (!plain) total = group_sum<G>(total);
   if (t >= T_rows) return;
-  const float norm = renorm ? chosen : (act == MIX_ACT_SOFTMAX ? total : 1.f);
+  const float norm = plain ? 1.f : total;
 #pragma unroll
   for (int s = 0; s < S; ++s) {
     const int j = s * G + sub;
     if (j < k) {
       idx[t * k + j] = my_idx[s];
-      weights[t * k + j] = my_idx[s] >= 0 ? my_e[s] / norm : 0.f;
+      weights[t * k + j] = my_idx[s] >= 0 ? my_x[s] / norm : 0.f;
     }
   }
 }
@@ -106,17 +141,26 @@ router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_ro
 //   sigmoid                dx_i = w_i (1 - sigmoid(x_i)) g_i    at the chosen experts
 //   sigmoid, renormalised  dx_i = w_i (1 - sigmoid(x_i)) (g_i - s)
 // Entries without an expert are not read further: what stands in their d_w (NaN, say) does not matter.
+//
+// The chosen entries are spread over the row through shared memory where a lane has one of them (more than 64 experts): each lane
+// puts its own where its column is, and the row comes back in the lanes' pieces.  Narrower rows compare each entry with each
+// column of a lane, for 32 / G rows at a time.
 template <typename T, int G, int V>
 __global__ void __launch_bounds__(kSelThreads)
 router_topk_grad_kernel(const T* __restrict__ logits, long long ld, int vec, int T_rows, int E, int k, int act, int renorm,
                         const int* __restrict__ idx, const float* __restrict__ weights, const float* __restrict__ d_weights,
                         T* __restrict__ d_logits, long long ld_d, int vec_d) {
   constexpr int S = G >= kOpMaxTopk ? 1 : (G == 1 ? 8 : kOpMaxTopk / G);
+  __shared__ float4 spread[S == 1 ? kSelThreads * V / 4 : 1];
   pdl_wait();
   pdl_launch_dependents();
   const int sub = threadIdx.x & (G - 1);
   const long long t = ((long long)blockIdx.x * kSelThreads + threadIdx.x) / G;
-  const bool row = t < T_rows;
+  const bool row = t < T_rows, dense = act == MIX_ACT_SOFTMAX && !renorm;
+  float d[V], p[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) p[v] = -INFINITY;
+  if (dense && row) load_row<T, G, V>(logits + t * ld, E, sub, vec != 0, p);
   int my_idx[S];
   float my_g[S], my_w[S];
   float s = 0.f;
@@ -133,48 +177,60 @@ router_topk_grad_kernel(const T* __restrict__ logits, long long ld, int vec, int
     any |= ok;
   }
   s = group_sum<G>(s);
-  any = group_max<G>(any ? 1.f : 0.f) > 0.f;
-  float d[V];
-  float p[V];
-  const bool dense = act == MIX_ACT_SOFTMAX && !renorm;
-#pragma unroll
-  for (int v = 0; v < V; ++v) d[v] = 0.f;
   if (dense) {
-    if (row && any) {
-      load_row<T, G, V>(logits + t * ld, E, sub, vec != 0, p);
-    } else {
-#pragma unroll
-      for (int v = 0; v < V; ++v) p[v] = -INFINITY;
-    }
-    float top = p[0];
-#pragma unroll
-    for (int v = 1; v < V; ++v) top = fmaxf(top, p[v]);
-    top = group_max<G>(top);
-    float total = 0.f;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      p[v] = score_softmax(p[v], top);
-      total += p[v];
-    }
-    total = group_sum<G>(total);
-    const float inv = total > 0.f ? 1.f / total : 0.f;
+    any = group_any<G>(any);
+    const float total = group_sum<G>(scores<V>(act, group_max<G>(top_of<V>(p)), p));
+    const float inv = any && total > 0.f ? 1.f / total : 0.f;
 #pragma unroll
     for (int v = 0; v < V; ++v) p[v] *= inv;
   } else {
 #pragma unroll
     for (int i = 0; i < S; ++i) {
       float g = my_w[i] * ((act == MIX_ACT_SOFTMAX || renorm) ? my_g[i] - s : my_g[i]);
-      if (act == MIX_ACT_SIGMOID && my_idx[i] >= 0) g *= sigmoidf(-to_f32(logits[t * ld + my_idx[i]]));
+      if (act == MIX_ACT_SIGMOID && my_idx[i] >= 0) g *= sigmoid_row(-to_f32(logits[t * ld + my_idx[i]]));
       my_g[i] = my_idx[i] >= 0 ? g : 0.f;
     }
   }
+  if (S == 1) {
+    constexpr int VW = RowVec<T>::VW;
+    const int lane = threadIdx.x & 31;
+    float* buf = reinterpret_cast<float*>(spread) + (threadIdx.x / G) * (G * V);
+    // lane `sub`'s piece b of the row begins at column b * G * VW + sub * VW
 #pragma unroll
-  for (int j = 0; j < (G == 1 ? 8 : kOpMaxTopk); ++j) {
-    if (j >= k) break;
-    const int at = __shfl_sync(0xffffffffu, my_idx[j / G], j % G, G);
-    const float g = __shfl_sync(0xffffffffu, my_g[j / G], j % G, G);
+    for (int b = 0; b < V / 4; ++b)
+      *reinterpret_cast<float4*>(buf + (b * 4 / VW) * (G * VW) + sub * VW + (b * 4) % VW) = make_float4(0.f, 0.f, 0.f, 0.f);
+    // the same expert twice in a row (never in what the selection gives): its entries are added in their order
+    const unsigned same = __match_any_sync(0xffffffffu, my_idx[0] < 0 ? -1 - lane : my_idx[0] + (lane / G) * kOpMaxExperts);
+    float g = my_g[0];
+    if (__any_sync(0xffffffffu, (same & (same - 1u)) != 0u)) {
+      g = 0.f;
+      for (int i = 0; i < 32; ++i) {
+        const float x = __shfl_sync(0xffffffffu, my_g[0], i);
+        if ((same >> i) & 1u) g += x;
+      }
+    }
+    __syncwarp();
+    if (my_idx[0] >= 0 && lane == __ffs(same) - 1) buf[my_idx[0]] = g;
+    __syncwarp();
 #pragma unroll
-    for (int v = 0; v < V; ++v) d[v] += row_col<T, G>(v, sub) == at ? g : 0.f;
+    for (int b = 0; b < V / 4; ++b) {
+      const float4 f = *reinterpret_cast<const float4*>(buf + (b * 4 / VW) * (G * VW) + sub * VW + (b * 4) % VW);
+      d[4 * b] = f.x;
+      d[4 * b + 1] = f.y;
+      d[4 * b + 2] = f.z;
+      d[4 * b + 3] = f.w;
+    }
+  } else {
+#pragma unroll
+    for (int v = 0; v < V; ++v) d[v] = 0.f;
+#pragma unroll
+    for (int j = 0; j < (G == 1 ? 8 : kOpMaxTopk); ++j) {
+      if (j >= k) break;
+      const int at = __shfl_sync(0xffffffffu, my_idx[j / G], j % G, G);
+      const float g = __shfl_sync(0xffffffffu, my_g[j / G], j % G, G);
+#pragma unroll
+      for (int v = 0; v < V; ++v) d[v] += row_col<T, G>(v, sub) == at ? g : 0.f;
+    }
   }
   if (dense) {
 #pragma unroll
@@ -190,6 +246,7 @@ constexpr int kOrdSteps = 8;                                    // entries a lan
 constexpr int kOrdChunk = kOrdThreads * kOrdSteps;              // entries a CTA takes
 constexpr int kOrdBuckets = kOpMaxExperts + 1;                  // the last of a call's holds the entries without an expert
 
+__host__ __device__ constexpr int hist_stride(int E) { return (E + 1 + 3) & ~3; }   // counts of a chunk, in whole 16-byte vectors
 __device__ __forceinline__ int bucket_of(int i, int E) { return (unsigned)i < (unsigned)E ? i : E; }
 
 __global__ void __launch_bounds__(kOrdThreads)
@@ -206,7 +263,7 @@ expert_hist_kernel(const int* __restrict__ idx, int n, int E, int* __restrict__ 
     if (at < n) atomicAdd(&h[bucket_of(idx[at], E)], 1);
   }
   __syncthreads();
-  for (int e = threadIdx.x; e <= E; e += kOrdThreads) hist[(size_t)blockIdx.x * (E + 1) + e] = h[e];
+  for (int e = threadIdx.x; e < hist_stride(E); e += kOrdThreads) hist[(size_t)blockIdx.x * hist_stride(E) + e] = e <= E ? h[e] : 0;
 }
 
 // Entry i of the CTA's chunk goes to  (entries of lower experts) + (entries of this expert in earlier chunks, in earlier warps
@@ -246,19 +303,25 @@ expert_order_kernel(const int* __restrict__ idx, int n, int E, const int* __rest
     __syncwarp();
   }
   __syncthreads();
-  if (n_chunks > 1) {                                    // columns side by side, the chunks dealt to the threads left over
-    const int wide = min((E + 1 + 31) & ~31, kOrdThreads), lanes = kOrdThreads / wide;
-    const int part = threadIdx.x / wide;
-    for (int e = part < lanes ? threadIdx.x % wide : E + 1; e <= E; e += wide) {
-      int sum = 0, pre = 0;
+  if (n_chunks > 1) {                                    // four columns a thread, the chunks dealt to the threads left over
+    const int wide = hist_stride(E) / 4, parts = kOrdThreads / wide, part = threadIdx.x / wide, col = threadIdx.x % wide;
+    if (part < parts) {
+      const int4* rows = reinterpret_cast<const int4*>(hist) + col;
+      int4 sum = make_int4(0, 0, 0, 0), pre = make_int4(0, 0, 0, 0);
 #pragma unroll 8
-      for (int c = part; c < n_chunks; c += lanes) {
-        const int h = hist[(size_t)c * (E + 1) + e];
-        sum += h;
-        pre += c < (int)blockIdx.x ? h : 0;
+      for (int c = part; c < n_chunks; c += parts) {
+        const int4 h = rows[(size_t)c * wide];
+        const int in = c < (int)blockIdx.x ? -1 : 0;
+        sum.x += h.x; sum.y += h.y; sum.z += h.z; sum.w += h.w;
+        pre.x += h.x & in; pre.y += h.y & in; pre.z += h.z & in; pre.w += h.w & in;
       }
-      atomicAdd(&total[e], sum);
-      atomicAdd(&before[e], pre);
+      const int s4[4] = {sum.x, sum.y, sum.z, sum.w}, p4[4] = {pre.x, pre.y, pre.z, pre.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (4 * col + i <= E) {
+          atomicAdd(&total[4 * col + i], s4[i]);
+          atomicAdd(&before[4 * col + i], p4[i]);
+        }
     }
   }
   __syncthreads();
@@ -384,7 +447,7 @@ extern "C" int mix_router_topk_grad(const void* logits, int dtype, long long ld,
 extern "C" long long mix_expert_order_workspace(long long n, int n_experts) {
   if (n < 0 || n > MIX_ORDER_MAX_ENTRIES || n_experts < 1 || n_experts > kOpMaxExperts) return MIX_ERR_OUT_OF_RANGE;
   const long long chunks = (n + kOrdChunk - 1) / kOrdChunk;
-  return chunks > 1 ? chunks * (n_experts + 1) * (long long)sizeof(int) : 0;
+  return chunks > 1 ? chunks * hist_stride(n_experts) * (long long)sizeof(int) : 0;
 }
 
 extern "C" int mix_expert_order(const int* idx, long long n, int n_experts, int* offsets, int* order, int* position, void* workspace,
@@ -393,8 +456,8 @@ extern "C" int mix_expert_order(const int* idx, long long n, int n_experts, int*
   if (n < 0 || n > MIX_ORDER_MAX_ENTRIES) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "n %lld outside [0, %d]", n, MIX_ORDER_MAX_ENTRIES);
   if (!offsets || (n > 0 && (!idx || !order || !position))) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "idx, offsets, order and position are required");
   const long long need = mix_expert_order_workspace(n, n_experts);
-  if (need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 3u)))
-    MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "the workspace has to hold %lld bytes, on 4 bytes", need);
+  if (need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15u)))
+    MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "the workspace has to hold %lld bytes, on 16 bytes", need);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   int* hist = static_cast<int*>(workspace);
   const int chunks = n == 0 ? 1 : (int)((n + kOrdChunk - 1) / kOrdChunk);

@@ -139,9 +139,10 @@ def reach(x):
 
 
 def rel_p(x, act):
-    """Relative bound on a probability: the argument of each exponential is off by U times its size, the exponential itself by
-    two steps (4 U), a sigmoid by its sum and division (3 U); numerator and denominator both, the sum of up to 512 terms in a
-    tree behind 16 serial ones 24 U, the division and the multiplication that follow 4 U."""
+    """Relative bound on a probability.  e^d, d = x - top: the difference and the exponent's argument are off by half a step of d
+    each and the exponential by two steps, (2 |d| + 4) U.  The sum of up to 512 such terms is off by their mean, weighted by p --
+    sum p |d| is at most the entropy, ln 512 < 6.3 -- that is 17 U, and by 24 U of additions (a tree behind 16 serial ones);
+    reciprocal and products 4 U.  A sigmoid's own steps (an addition and a reciprocal, 3 U) stand in the place of the difference's."""
     return (2 * (reach(x) + 8) + 32) * U
 
 
