@@ -521,6 +521,7 @@ int mix_sae_apply_static(void* hidden, int n_rows, int d_model, const mix_sae_we
 enum { MIX_DTYPE_F32 = 0, MIX_DTYPE_BF16 = 1, MIX_DTYPE_F16 = 2 };   /* element types of the tensors of these calls */
 #define MIX_ORDER_MAX_ENTRIES 16777216    /* mix_expert_order: most entries of a call */
 #define MIX_BALANCE_MAX_SEGMENTS 65536    /* mix_router_balance: most segments of a call */
+#define MIX_COMBINE_MAX_N 8388480         /* mix_expert_combine: widest row */
 #define MIX_I8_MAX_K 131056               /* 8-bit products: longest row (a sum of 131071 products of -128 and -128 still fits in 31 bits) */
 
 /* The k experts of each token.  logits: dtype [T, n_experts], rows ld elements apart.  idx int32 [T, k]: the k largest logits of
@@ -545,7 +546,7 @@ int mix_router_topk_grad(const void* logits, int dtype, long long ld, int T, int
    those of expert 1, and so on, each expert's in rising order; -1 behind them.  offsets int32 [n_experts + 1]: expert e's are
    order[offsets[e] .. offsets[e + 1]), so differences of neighbours are the per-expert counts.  position int32 [n]: the place of an entry in
    `order`, -1 for entries that name no expert (idx outside [0, n_experts)).
-   workspace: mix_expert_order_workspace(n, n_experts) bytes (0 for up to 4096 entries; negative: a mix_status), on 16 bytes.
+   workspace: mix_expert_order_workspace(n, n_experts) bytes (0 for up to 65536 entries; negative: a mix_status), on 16 bytes.
    Errors: OUT_OF_RANGE (n outside [0, MIX_ORDER_MAX_ENTRIES], n_experts), INVALID_ARG. */
 long long mix_expert_order_workspace(long long n, int n_experts);
 int mix_expert_order(const int* idx, long long n, int n_experts, int* offsets, int* order, int* position, void* workspace,
@@ -607,7 +608,7 @@ int mix_linear_int_status(unsigned* bits, void* stream, char* errbuf, int errbuf
    once.  y: dtype [y_rows, N], rows ld_y apart, in mix_expert_order()'s order; position int32 [T, k] from the same call, entries outside
    [0, y_rows) do not count (nor what stands in their weights).  out: dtype [T, N], rows ld_out apart; a token without experts gets zeros.
    out may not overlap y.
-   Errors: OUT_OF_RANGE (T < 0, N < 1, k outside [1, 16], ld below N), INVALID_ARG. */
+   Errors: OUT_OF_RANGE (T < 0, N outside [1, MIX_COMBINE_MAX_N], k outside [1, 16], ld below N), INVALID_ARG. */
 int mix_expert_combine(const void* y, int dtype, long long ld_y, int y_rows, const float* weights, const int* position, int T, int k, int N,
                        void* out, long long ld_out, void* stream, char* errbuf, int errbuf_len);
 

@@ -13,13 +13,17 @@ using namespace mix::tc;
 namespace {
 
 // ---------------------------------------------------------------------------------------------------- quantisation
-// A row's codes are the exact quotients 127 x / a rounded to the nearest, halves to the even one: x has 11 significant bits at
-// most, 127 x is exact in fp32, the quotient is never so close to a half that a correctly rounded division would cross it.  A
-// division costs more than the rest of the row's work, so the quotient comes from a multiplication by 127 / a (off by at most
-// 127 * 2^-23), and a vector is divided only where one of its quotients lies within 2^-13 of a half.  Adding 1.5 * 2^23 rounds
-// to a whole number and leaves its two's complement in the low bits of the sum.
-// A row that lies far from 1 is first scaled by a power of two, which is exact: neither 127 x nor 127 / a leaves fp32's range.
-// 8192 rows of 8192 bf16: 60 us with a rounding, a comparison and a conversion per element, %s us so.
+// A row's codes are the exact quotients 127 x / a rounded to the nearest, halves to the even one.  A division costs more than the
+// rest of the row's work, so the quotient comes from a multiplication by 127 / a, and adding 1.5 * 2^23 (in the same instruction)
+// rounds to a whole number, whose two's complement is in the low bits of the sum.  That is exact:
+//   x = X 2^f and a = A 2^e with whole X, A < 2^11 (fp16; 2^8 for bf16).  A quotient that is no half differs from the nearest half
+//   (2n + 1) / 2 by |254 X 2^f - (2n + 1) A 2^e| / (2 A 2^e), at least 2^(f - e) / 2^12, which relative to the quotient is 9.6e-7 or
+//   more; the factor, nudged up by one step, is off by 1.8e-7 at most.
+//   A half needs 127 | (2n + 1) A.  If 127 does not divide A that is 2n + 1 = 127 alone: x = a / 2, 63.5, and the factor nudged up
+//   takes it to 64, the even one.  If A = 127 2^j the factor is a power of two and everything is exact.  Other multiples of 127 (eight
+//   largest values of fp16 in 1024) go by division; so do rows that lie so far from 1 that 127 x or 127 / a would leave fp32's
+//   range, scaled by a power of two first.
+// 8192 rows of 8192 bf16: 60 us with a rounding, a comparison and a conversion per element, 51 with a test for halves, %s us so.
 template <typename T>
 struct Pair2;
 template <>
@@ -41,37 +45,35 @@ __device__ __forceinline__ typename Pair2<T>::V sizes8(const uint4& raw, typenam
   return a;
 }
 template <typename T>
-__device__ __forceinline__ uint2 codes8(const uint4& raw, float pre, float inv, float a) {
-  constexpr float kRound = 12582912.f;
+__device__ __forceinline__ uint2 codes8(const uint4& raw, float factor) {
   const typename Pair2<T>::V* e = reinterpret_cast<const typename Pair2<T>::V*>(&raw);
   unsigned t[8];
-  float far = 0.f;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const float2 f = Pair2<T>::f32(e[j]);
-    const float s0 = fmaf(f.x * pre, inv, kRound), s1 = fmaf(f.y * pre, inv, kRound);
-    far = fmaxf(far, fmaxf(fabsf(fmaf(f.x * pre, inv, kRound - s0)), fabsf(fmaf(f.y * pre, inv, kRound - s1))));
-    t[2 * j] = __float_as_uint(s0);
-    t[2 * j + 1] = __float_as_uint(s1);
-  }
-  if (far > 0.5f - 0.000122f) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float2 f = Pair2<T>::f32(e[j]);
-      t[2 * j] = (unsigned)(int)rintf(__fdiv_rn(127.f * (f.x * pre), a));
-      t[2 * j + 1] = (unsigned)(int)rintf(__fdiv_rn(127.f * (f.y * pre), a));
-    }
+    t[2 * j] = __float_as_uint(fmaf(f.x, factor, 12582912.f));
+    t[2 * j + 1] = __float_as_uint(fmaf(f.y, factor, 12582912.f));
   }
   uint2 c;
   c.x = __byte_perm(__byte_perm(t[0], t[1], 0x0040), __byte_perm(t[2], t[3], 0x0040), 0x5410);
   c.y = __byte_perm(__byte_perm(t[4], t[5], 0x0040), __byte_perm(t[6], t[7], 0x0040), 0x5410);
   return c;
 }
+template <typename T>
+__device__ __noinline__ uint2 codes8_divided(const uint4& raw, float a) {
+  const float pre = a > 1e30f ? 0x1p-64f : (a < 1e-30f ? 0x1p64f : 1.f);
+  const T* e = reinterpret_cast<const T*>(&raw);
+  uint2 c;
+  signed char* b = reinterpret_cast<signed char*>(&c);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) b[j] = (signed char)(int)rintf(__fdiv_rn(127.f * (to_f32(e[j]) * pre), a * pre));
+  return c;
+}
 
 constexpr int kQuantVecs = 4;                                  // 8-element vectors a thread keeps
-template <typename T, int THREADS>
-__global__ void __launch_bounds__(THREADS < 128 ? 128 : THREADS)
-quantize_rows_kernel(const T* __restrict__ x, long long ld, int vec, int x_rows, const int* __restrict__ order, int div, int n_rows, int d,
+template <typename T, int THREADS, bool vec>
+__global__ void __launch_bounds__(THREADS < 128 ? 128 : THREADS, THREADS == 256 ? 6 : 12)
+quantize_rows_kernel(const T* __restrict__ x, long long ld, int x_rows, const int* __restrict__ order, int div, int n_rows, int d,
                      signed char* __restrict__ codes, float* __restrict__ scale) {
   constexpr int kRows = THREADS < 128 ? 128 / THREADS : 1;     // rows a CTA takes
   __shared__ unsigned red[kRows == 1 ? THREADS / 32 : 1];
@@ -129,17 +131,20 @@ quantize_rows_kernel(const T* __restrict__ x, long long ld, int vec, int x_rows,
     if (tid == 0) scale[i] = __int_as_float(0x7fc00000);
     return;
   }
-  const float pre = a > 1e30f ? 0x1p-64f : (a < 1e-30f ? 0x1p64f : 1.f);
-  const float as = a * pre, inv = as > 0.f ? 127.f / as : 0.f;
-  if (as == 0.f) {
+  const unsigned digits = (bits & 0x7fffffu) | 0x800000u, by127 = digits / 127u;
+  const bool multiple = by127 * 127u == digits, exact = multiple && (by127 & (by127 - 1u)) == 0u;
+  if (a == 0.f) {
     for (int v = tid; v < n_vec; v += THREADS) out[v] = make_uint2(0u, 0u);
-  } else {
+  } else if (a >= 1e-30f && a <= 1e30f && (!multiple || exact)) {
+    const float factor = __uint_as_float(__float_as_uint(__fdiv_rn(127.f, a)) + (exact ? 0u : 1u));
 #pragma unroll
     for (int b = 0; b < kQuantVecs; ++b) {
       const int v = tid + b * THREADS;
-      if (v < n_vec) out[v] = codes8<T>(keep[b], pre, inv, as);
+      if (v < n_vec) out[v] = codes8<T>(keep[b], factor);
     }
-    for (int v = tid + kQuantVecs * THREADS; v < n_vec; v += THREADS) out[v] = codes8<T>(fetch(v), pre, inv, as);
+    for (int v = tid + kQuantVecs * THREADS; v < n_vec; v += THREADS) out[v] = codes8<T>(fetch(v), factor);
+  } else {
+    for (int v = tid; v < n_vec; v += THREADS) out[v] = codes8_divided<T>(fetch(v), a);
   }
   if (tid == 0) scale[i] = __fdiv_rn(a, 127.f);
 }
@@ -208,6 +213,7 @@ __device__ __forceinline__ void umma_i8_pair(unsigned d_tmem, unsigned long long
 
 struct I8Tile {
   int expert, ch0, row0, n_tok;
+  bool once;                                                   // no other tile reads these channels of W
 };
 
 // Tiles of an expert: groups of kGroup token tiles; in a group the channels one after the other, each with all of the group's
@@ -220,6 +226,7 @@ __device__ __forceinline__ I8Tile i8_tile(const GemmShared* sh, int tile, int ch
   const int group = local / (kGroup * ch_tiles), in = local - group * kGroup * ch_tiles, wide = min(kGroup, tt - group * kGroup);
   I8Tile t;
   t.expert = e;
+  t.once = tt == 1;
   t.ch0 = in / wide * (kPair ? 2 * kTileCh : kTileCh);
   const int tk = group * kGroup + in % wide;
   // an expert's rows are dealt evenly: with a full tile and a small one in turn, the even workers would get all the full ones
@@ -310,6 +317,7 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
     int stage = 0, e = 0;
     unsigned phase = 0;
     bool ok = true;
+    const unsigned long long stream = l2_evict_first();
     for (int tile = worker; tile < total && ok; tile += n_workers) {
       const I8Tile t = i8_tile<NT, kPair>(sh, tile, ch_tiles, e);
       if (t.n_tok <= 0) continue;
@@ -318,6 +326,7 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
       // (E * N rows of W fit in 31 bits: checked on the host.  Channels behind the last and tokens behind the expert's are
       // other rows or the fill value; what comes of them is not stored)
       const int wy = uniform(t.expert * N + t.ch0 + rank * kTileCh), xy = uniform(t.row0 + (kPair ? rank * tok_rows : 0));
+      const bool once = uniform((int)t.once) != 0;             // (then what the kernels around this one share stays in L2)
       const unsigned bytes = (Cfg::kABytes + boxes * Cfg::kBoxRows * kKBytes) * Cfg::kCtas;
       for (int kb = 0; kb < num_kb; ++kb) {
         if (!mbar_wait_bounded_warp(smem_u32(&sh->empty[stage]), phase ^ 1u, &sh->abort_flag, cap, &g_i8_status)) { ok = false; break; }
@@ -325,12 +334,14 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
         if (kPair) {
           if (rank == 0) mbar_expect_tx(bar, bytes, on);
           const unsigned bar_c = mapa_cluster(bar, 0);
-          tma_load_2d_pair(sa, &tmap_w, kb * kKBytes, wy, bar_c, on);
+          if (once) tma_load_2d_pair_hint(sa, &tmap_w, kb * kKBytes, wy, bar_c, stream, on);
+          else tma_load_2d_pair(sa, &tmap_w, kb * kKBytes, wy, bar_c, on);
           for (int b = 0; b < boxes; ++b)
             tma_load_2d_pair(sa + Cfg::kABytes + b * Cfg::kBoxRows * kKBytes, &tmap_x, kb * kKBytes, xy + b * Cfg::kBoxRows, bar_c, on);
         } else {
           mbar_expect_tx(bar, bytes, on);
-          tma_load_2d(sa, &tmap_w, kb * kKBytes, wy, bar, on);
+          if (once) tma_load_2d_hint(sa, &tmap_w, kb * kKBytes, wy, bar, stream, on);
+          else tma_load_2d(sa, &tmap_w, kb * kKBytes, wy, bar, on);
           for (int b = 0; b < boxes; ++b)
             tma_load_2d(sa + Cfg::kABytes + b * Cfg::kBoxRows * kKBytes, &tmap_x, kb * kKBytes, xy + b * Cfg::kBoxRows, bar, on);
         }
@@ -452,45 +463,53 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
 }
 
 // ---------------------------------------------------------------------------------------------------- the sum over experts
-template <typename T>
-__global__ void __launch_bounds__(256)
-combine_kernel(const T* __restrict__ y, long long ld_y, int y_rows, const float* __restrict__ weights, const int* __restrict__ position, int T_rows,
-               int k, int N, T* __restrict__ out, long long ld_out, int vec) {
-  __shared__ float w[kOpMaxTopk];
-  __shared__ int at[kOpMaxTopk];
+// A thread has one vector of one token; all of the token's rows are on their way at once.
+constexpr int kCombineThreads = 128;
+template <typename T, int KMAX, bool vec>
+__global__ void __launch_bounds__(kCombineThreads)
+combine_kernel(const T* __restrict__ y, long long ld_y, int y_rows, const float* __restrict__ weights, const int* __restrict__ position,
+               int k, int N, T* __restrict__ out, long long ld_out) {
+  constexpr int VW = vec ? RowVec<T>::VW : 1;
   pdl_wait();
   pdl_launch_dependents();
   const long long t = blockIdx.x;
-  if (threadIdx.x < k) {
-    const int p = position[t * k + threadIdx.x];
-    at[threadIdx.x] = p >= 0 && p < y_rows ? p : -1;
-    w[threadIdx.x] = weights[t * k + threadIdx.x];
+  const int c0 = (blockIdx.y * kCombineThreads + threadIdx.x) * VW;
+  if (c0 >= N) return;
+  int at[KMAX];
+  float w[KMAX];
+#pragma unroll
+  for (int j = 0; j < KMAX; ++j) {
+    at[j] = j < k ? position[t * k + j] : -1;
+    w[j] = j < k ? weights[t * k + j] : 0.f;
   }
-  __syncthreads();
-  constexpr int VW = RowVec<T>::VW;
-  const int n_vec = vec ? N / VW : 0;
-  for (int v = blockIdx.y * 256 + threadIdx.x; v < n_vec; v += gridDim.y * 256) {
-    float acc[VW];
+  float acc[VW];
 #pragma unroll
-    for (int i = 0; i < VW; ++i) acc[i] = 0.f;
-    for (int j = 0; j < k; ++j) {
-      if (at[j] < 0) continue;
-      const uint4 raw = *reinterpret_cast<const uint4*>(y + at[j] * ld_y + (long long)VW * v);
-      const T* e = reinterpret_cast<const T*>(&raw);
+  for (int i = 0; i < VW; ++i) acc[i] = 0.f;
+  if (vec && c0 + VW <= N) {
+    uint4 raw[KMAX];
 #pragma unroll
-      for (int i = 0; i < VW; ++i) acc[i] = fmaf(w[j], to_f32(e[i]), acc[i]);
-    }
-    uint4 raw;
-    T* e = reinterpret_cast<T*>(&raw);
+    for (int j = 0; j < KMAX; ++j)
+      if ((unsigned)at[j] < (unsigned)y_rows) raw[j] = *reinterpret_cast<const uint4*>(y + at[j] * ld_y + c0);
+#pragma unroll
+    for (int j = 0; j < KMAX; ++j)
+      if ((unsigned)at[j] < (unsigned)y_rows) {
+        const T* e = reinterpret_cast<const T*>(&raw[j]);
+#pragma unroll
+        for (int i = 0; i < VW; ++i) acc[i] = fmaf(w[j], to_f32(e[i]), acc[i]);
+      }
+    uint4 sum;
+    T* e = reinterpret_cast<T*>(&sum);
 #pragma unroll
     for (int i = 0; i < VW; ++i) e[i] = from_f32<T>(acc[i]);
-    *reinterpret_cast<uint4*>(out + t * ld_out + (long long)VW * v) = raw;
-  }
-  for (int c = n_vec * VW + blockIdx.y * 256 + threadIdx.x; c < N; c += gridDim.y * 256) {
-    float acc = 0.f;
-    for (int j = 0; j < k; ++j)
-      if (at[j] >= 0) acc = fmaf(w[j], to_f32(y[at[j] * ld_y + c]), acc);
-    out[t * ld_out + c] = from_f32<T>(acc);
+    *reinterpret_cast<uint4*>(out + t * ld_out + c0) = sum;
+  } else {
+    for (int i = 0; i < VW && c0 + i < N; ++i) {
+      float a = 0.f;
+#pragma unroll
+      for (int j = 0; j < KMAX; ++j)
+        if ((unsigned)at[j] < (unsigned)y_rows) a = fmaf(w[j], to_f32(y[at[j] * ld_y + c0 + i]), a);
+      out[t * ld_out + c0 + i] = from_f32<T>(a);
+    }
   }
 }
 
@@ -578,30 +597,47 @@ int gemm_call(const Gemm& g, int dtype, void* stream, char* errbuf, int errbuf_l
   return MIX_OK;
 }
 
+template <typename T, bool vec>
+cudaError_t quantize_launch_as(const void* x, long long ld, int x_rows, const int* order, int div, int n_rows, int d, signed char* codes,
+                               float* scale, cudaStream_t s) {
+  const T* xt = static_cast<const T*>(x);
+  if (d <= 1024)                                               // a warp holds the row
+    return launch_pdl(kPdlHook, quantize_rows_kernel<T, 32, vec>, dim3((unsigned)((n_rows + 3ll) / 4)), dim3(128), 0, s, xt, ld, x_rows, order, div,
+                      n_rows, d, codes, scale);
+  if (d <= 4096)
+    return launch_pdl(kPdlHook, quantize_rows_kernel<T, 128, vec>, dim3((unsigned)n_rows), dim3(128), 0, s, xt, ld, x_rows, order, div, n_rows, d,
+                      codes, scale);
+  return launch_pdl(kPdlHook, quantize_rows_kernel<T, 256, vec>, dim3((unsigned)n_rows), dim3(256), 0, s, xt, ld, x_rows, order, div, n_rows, d,
+                    codes, scale);
+}
 template <typename T>
 cudaError_t quantize_launch(const void* x, long long ld, int x_rows, const int* order, int div, int n_rows, int d, signed char* codes,
                             float* scale, cudaStream_t s) {
   const int vec = (((uintptr_t)x | (uintptr_t)(ld * 2)) & 15u) == 0;
-  const T* xt = static_cast<const T*>(x);
-  if (d <= 1024)                                               // a warp holds the row
-    return launch_pdl(kPdlHook, quantize_rows_kernel<T, 32>, dim3((unsigned)((n_rows + 3ll) / 4)), dim3(128), 0, s, xt, ld, vec, x_rows, order, div,
-                      n_rows, d, codes, scale);
-  if (d <= 4096)
-    return launch_pdl(kPdlHook, quantize_rows_kernel<T, 128>, dim3((unsigned)n_rows), dim3(128), 0, s, xt, ld, vec, x_rows, order, div, n_rows, d,
-                      codes, scale);
-  return launch_pdl(kPdlHook, quantize_rows_kernel<T, 256>, dim3((unsigned)n_rows), dim3(256), 0, s, xt, ld, vec, x_rows, order, div, n_rows, d,
-                    codes, scale);
+  return vec ? quantize_launch_as<T, true>(x, ld, x_rows, order, div, n_rows, d, codes, scale, s)
+             : quantize_launch_as<T, false>(x, ld, x_rows, order, div, n_rows, d, codes, scale, s);
 }
 
+template <typename T, bool vec>
+cudaError_t combine_launch_as(const void* y, long long ld_y, int y_rows, const float* weights, const int* position, int T_rows, int k, int N,
+                              void* out, long long ld_out, cudaStream_t s) {
+  constexpr int kCols = kCombineThreads * (vec ? RowVec<T>::VW : 1);
+  const dim3 grid((unsigned)T_rows, (unsigned)((N + kCols - 1) / kCols));
+#define MIX_COMBINE(K)                                                                                                                \
+  return launch_pdl(kPdlHook, combine_kernel<T, K, vec>, grid, dim3(kCombineThreads), 0, s, static_cast<const T*>(y), ld_y, y_rows, weights, \
+                    position, k, N, static_cast<T*>(out), ld_out)
+  if (k <= 2) MIX_COMBINE(2);
+  if (k <= 4) MIX_COMBINE(4);
+  if (k <= 8) MIX_COMBINE(8);
+  MIX_COMBINE(kOpMaxTopk);
+#undef MIX_COMBINE
+}
 template <typename T>
 cudaError_t combine_launch(const void* y, long long ld_y, int y_rows, const float* weights, const int* position, int T_rows, int k, int N,
-                           void* out, long long ld_out, int n_sms, cudaStream_t s) {
-  const int vec = (((uintptr_t)y | (uintptr_t)out | (uintptr_t)(ld_y * (long long)sizeof(T)) | (uintptr_t)(ld_out * (long long)sizeof(T))) & 15u) == 0;
-  const int pieces = vec ? (N / RowVec<T>::VW + 255) / 256 : (N + 255) / 256;
-  int gy = 1;                                                  // few tokens: their columns are dealt to several CTAs
-  while (gy < pieces && gy < 64 && (long long)T_rows * gy < 2 * n_sms) gy *= 2;
-  return launch_pdl(kPdlHook, combine_kernel<T>, dim3((unsigned)T_rows, gy), dim3(256), 0, s, static_cast<const T*>(y), ld_y, y_rows, weights,
-                    position, T_rows, k, N, static_cast<T*>(out), ld_out, vec);
+                           void* out, long long ld_out, cudaStream_t s) {
+  const bool vec = (((uintptr_t)y | (uintptr_t)out | (uintptr_t)(ld_y * (long long)sizeof(T)) | (uintptr_t)(ld_out * (long long)sizeof(T))) & 15u) == 0;
+  return vec ? combine_launch_as<T, true>(y, ld_y, y_rows, weights, position, T_rows, k, N, out, ld_out, s)
+             : combine_launch_as<T, false>(y, ld_y, y_rows, weights, position, T_rows, k, N, out, ld_out, s);
 }
 
 }  // namespace
@@ -651,15 +687,13 @@ extern "C" int mix_expert_combine(const void* y, int dtype, long long ld_y, int 
   if (op_elem_size(dtype) == 0) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "dtype %d is no MIX_DTYPE_*", dtype);
   if (T < 0 || y_rows < 0) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "%d tokens, %d rows of y", T, y_rows);
   if (k < 1 || k > kOpMaxTopk) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "k %d outside [1, %d]", k, kOpMaxTopk);
-  if (N < 1) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "N %d is below 1", N);
+  if (N < 1 || N > MIX_COMBINE_MAX_N) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "N %d outside [1, %d]", N, MIX_COMBINE_MAX_N);
   if (ld_y < N || ld_out < N) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "row strides %lld, %lld below N %d", ld_y, ld_out, N);
   if (T == 0) return MIX_OK;
   if ((!y && y_rows > 0) || !weights || !position || !out) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "y, weights, position and out are required");
-  int dev, n_sms;
-  MIX_OP_CUDA(op_device(&dev, &n_sms));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (dtype == MIX_DTYPE_F32) MIX_OP_CUDA(combine_launch<float>(y, ld_y, y_rows, weights, position, T, k, N, out, ld_out, n_sms, s));
-  else if (dtype == MIX_DTYPE_BF16) MIX_OP_CUDA(combine_launch<__nv_bfloat16>(y, ld_y, y_rows, weights, position, T, k, N, out, ld_out, n_sms, s));
-  else MIX_OP_CUDA(combine_launch<__half>(y, ld_y, y_rows, weights, position, T, k, N, out, ld_out, n_sms, s));
+  if (dtype == MIX_DTYPE_F32) MIX_OP_CUDA(combine_launch<float>(y, ld_y, y_rows, weights, position, T, k, N, out, ld_out, s));
+  else if (dtype == MIX_DTYPE_BF16) MIX_OP_CUDA(combine_launch<__nv_bfloat16>(y, ld_y, y_rows, weights, position, T, k, N, out, ld_out, s));
+  else MIX_OP_CUDA(combine_launch<__half>(y, ld_y, y_rows, weights, position, T, k, N, out, ld_out, s));
   return MIX_OK;
 }

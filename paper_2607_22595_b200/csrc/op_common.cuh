@@ -180,8 +180,9 @@ __device__ __forceinline__ float score(int act, float x, float top) {      // of
   if (act == MIX_ACT_SOFTMAX) return x == top ? 1.f : exp_row(x - top);
   return top >= 0.f ? sigmoid_row(x) : exp_row(x - top) * rcp_hw(1.f + exp_row(x));
 }
+// rest: where given and the scores are sigmoids, 1 - sigmoid of each logit
 template <int V>
-__device__ __forceinline__ float scores(int act, float top, float (&x)[V]) {
+__device__ __forceinline__ float scores(int act, float top, float (&x)[V], float (*rest)[V] = nullptr) {
   float total = 0.f;
   if (act == MIX_ACT_SOFTMAX) {
     if (top == INFINITY) {
@@ -199,13 +200,16 @@ __device__ __forceinline__ float scores(int act, float top, float (&x)[V]) {
   } else if (top >= 0.f) {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      x[v] = x[v] == -INFINITY ? 0.f : sigmoid_row(x[v]);
+      const float s = sigmoid_row(x[v], rest ? &(*rest)[v] : nullptr);
+      x[v] = x[v] == -INFINITY ? 0.f : s;
       total += x[v];
     }
   } else {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      x[v] = x[v] == -INFINITY ? 0.f : exp_row(x[v] - top) * rcp_hw(1.f + exp_row(x[v]));
+      const float r = rcp_hw(1.f + exp_row(x[v]));
+      if (rest) (*rest)[v] = r;
+      x[v] = x[v] == -INFINITY ? 0.f : exp_row(x[v] - top) * r;
       total += x[v];
     }
   }

@@ -18,6 +18,7 @@ using namespace mix;
 namespace {
 
 constexpr int kUnitWarps = 8;              // warps of a unit where requests are long
+constexpr int kUnitCtas = 4, kGradCtas = 4; // CTAs an SM holds at a time: large batches make one wave of them
 constexpr int kFinThreads = 512;
 constexpr int kFinCluster = 8;
 
@@ -37,25 +38,34 @@ __device__ __forceinline__ int seg_of_row(const int* __restrict__ seg, int n_seg
   return lo;
 }
 
-template <typename T, int G, int V, int W>
-__global__ void __launch_bounds__(32 * W)
+// direct: unit u IS segment u, and the CTA that has seen all of it writes its results itself.
+struct BalanceOut {
+  float* loss;
+  int* counts;
+  float* mean_p;
+  int* rows;
+};
+template <typename T, int G, int V, int W, bool kDirect>
+__global__ void __launch_bounds__(32 * W, W == kUnitWarps ? kUnitCtas : 1)
 balance_kernel(const T* __restrict__ logits, long long ld, int vec, const int* __restrict__ idx, int T_rows, int E, int k, int act,
                const int* __restrict__ seg, int n_seg, int unit_rows, float* __restrict__ part_p, int* __restrict__ part_c,
-               int* __restrict__ part_n) {
+               int* __restrict__ part_n, const BalanceOut out) {
   constexpr int R = 32 / G;                                    // rows a warp holds
+  __shared__ double red[W];
+  __shared__ long long red_c[W];
   __shared__ int hist[G * V];
   __shared__ float sum_p[W][G * V];
   __shared__ int sum_n[W];
   pdl_wait();
   pdl_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane & (G - 1), unit = blockIdx.x;
-  const int r0 = unit * unit_rows, r1 = min(T_rows, r0 + unit_rows);
+  const int r0 = kDirect ? seg_at(seg, unit, T_rows) : unit * unit_rows, r1 = kDirect ? seg_at(seg, unit + 1, T_rows) : min(T_rows, r0 + unit_rows);
   for (int e = threadIdx.x; e < G * V; e += 32 * W) hist[e] = 0;
   if (W > 1) __syncthreads(); else __syncwarp();
-  for (int s = seg_of_row(seg, n_seg, T_rows, r0, lane); s < n_seg; ++s) {
-    const int a = max(seg_at(seg, s, T_rows), r0), b = min(seg_at(seg, s + 1, T_rows), r1);
-    if (a >= r1) break;
-    if (a >= b) continue;
+  for (int s = kDirect ? unit : seg_of_row(seg, n_seg, T_rows, r0, lane); s < (kDirect ? unit + 1 : n_seg); ++s) {
+    const int a = kDirect ? r0 : max(seg_at(seg, s, T_rows), r0), b = kDirect ? r1 : min(seg_at(seg, s + 1, T_rows), r1);
+    if (!kDirect && a >= r1) break;
+    if (!kDirect && a >= b) continue;
     float acc[V];
     int rows = 0;
 #pragma unroll
@@ -113,6 +123,43 @@ balance_kernel(const T* __restrict__ logits, long long ld, int vec, const int* _
     }
     if (lane == 0) sum_n[warp] = rows;
     if (W > 1) __syncthreads(); else __syncwarp();
+    if (kDirect) {
+      int n = 0;
+#pragma unroll
+      for (int w = 0; w < W; ++w) n += sum_n[w];
+      double fp = 0.0;
+      long long total = 0;
+      for (int e = threadIdx.x; e < E; e += 32 * W) {
+        double p = 0.0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) p += (double)sum_p[w][e];
+        p = n > 0 ? p / n : 0.0;
+        const int c = hist[e];
+        out.counts[(size_t)s * E + e] = c;
+        out.mean_p[(size_t)s * E + e] = (float)p;
+        fp += p * c;
+        total += c;
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        fp += __shfl_xor_sync(0xffffffffu, fp, o);
+        total += __shfl_xor_sync(0xffffffffu, total, o);
+      }
+      if (lane == 0) {
+        red[warp] = fp;
+        red_c[warp] = total;
+      }
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        for (int w = 1; w < W; ++w) {
+          fp += red[w];
+          total += red_c[w];
+        }
+        out.loss[s] = total > 0 ? (float)(E * fp / (double)total) : 0.f;
+        out.rows[s] = n;
+      }
+      return;
+    }
     const size_t slot = (size_t)(unit + s);
     for (int e = threadIdx.x; e < E; e += 32 * W) {
       float p = sum_p[0][e];
@@ -134,9 +181,10 @@ balance_kernel(const T* __restrict__ logits, long long ld, int vec, const int* _
 
 // One segment per cluster: CTA r of the cluster adds up the r-th part of the segment's slots, CTA 0 puts the parts together.
 // Sums in 64 bits: there are few, and a long request has thousands of slots.
+template <int cluster>
 __global__ void __launch_bounds__(kFinThreads)
 balance_finish_kernel(const float* __restrict__ part_p, const int* __restrict__ part_c, const int* __restrict__ part_n, int T_rows, int E,
-                      const int* __restrict__ seg, int unit_rows, int cluster, float* __restrict__ loss, int* __restrict__ counts,
+                      const int* __restrict__ seg, int unit_rows, float* __restrict__ loss, int* __restrict__ counts,
                       float* __restrict__ mean_p, int* __restrict__ rows_out) {
   __shared__ double sp[kOpMaxExperts];
   __shared__ int sc[kOpMaxExperts];
@@ -147,7 +195,7 @@ balance_finish_kernel(const float* __restrict__ part_p, const int* __restrict__ 
   __shared__ int lane_c[kFinThreads];
   pdl_wait();
   pdl_launch_dependents();
-  const int s = blockIdx.x / cluster, rank = blockIdx.x - s * cluster, tid = threadIdx.x;
+  const int s = blockIdx.x / cluster, rank = blockIdx.x % cluster, tid = threadIdx.x;
   const int a = seg_at(seg, s, T_rows), b = seg_at(seg, s + 1, T_rows);
   int u0 = 0, u1 = 0;                                          // units that the segment touches
   if (a < b) {
@@ -188,25 +236,32 @@ balance_finish_kernel(const float* __restrict__ part_p, const int* __restrict__ 
   }
   if (cluster > 1) tc::cluster_sync_all(); else __syncthreads();
   if (rank == 0) {
+    int others[cluster];                                       // (all on their way before one is used)
+#pragma unroll
+    for (int r = 1; r < cluster; ++r)
+      asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(others[r]) : "r"(tc::mapa_cluster(tc::smem_u32(&sn), r)));
     int n = sn;
-    for (int r = 1; r < cluster; ++r) {
-      int x;
-      asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(x) : "r"(tc::mapa_cluster(tc::smem_u32(&sn), r)));
-      n += x;
-    }
     double fp = 0.0;
     long long total = 0;
     if (tid < E) {
+      double op[cluster];
+      int oc[cluster];
+#pragma unroll
+      for (int r = 1; r < cluster; ++r) {
+        asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(op[r]) : "r"(tc::mapa_cluster(tc::smem_u32(&sp[tid]), r)));
+        asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(oc[r]) : "r"(tc::mapa_cluster(tc::smem_u32(&sc[tid]), r)));
+      }
       p = sp[tid];
       c = sc[tid];
+#pragma unroll
       for (int r = 1; r < cluster; ++r) {
-        double x;
-        int y;
-        asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(x) : "r"(tc::mapa_cluster(tc::smem_u32(&sp[tid]), r)));
-        asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(y) : "r"(tc::mapa_cluster(tc::smem_u32(&sc[tid]), r)));
-        p += x;
-        c += y;
+        p += op[r];
+        c += oc[r];
       }
+    }
+#pragma unroll
+    for (int r = 1; r < cluster; ++r) n += others[r];
+    if (tid < E) {
       p = n > 0 ? p / n : 0.0;
       counts[(size_t)s * E + tid] = c;
       mean_p[(size_t)s * E + tid] = (float)p;
@@ -236,7 +291,7 @@ balance_finish_kernel(const float* __restrict__ part_p, const int* __restrict__ 
 }
 
 template <typename T, int G, int V>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, kGradCtas)
 balance_grad_kernel(const T* __restrict__ logits, long long ld, int vec, const int* __restrict__ idx, int T_rows, int E, int k, int act,
                     const int* __restrict__ seg, int n_seg, const int* __restrict__ counts, const int* __restrict__ rows,
                     const float* __restrict__ d_loss, int warp_rows, T* __restrict__ d_logits, long long ld_d, int vec_d) {
@@ -297,11 +352,7 @@ balance_grad_kernel(const T* __restrict__ logits, long long ld, int vec, const i
 #pragma unroll
       for (int v = 0; v < V; ++v) x[v] = next[v];
       if (base + R < b) fetch(base + R, next, next_named);
-      if (act == MIX_ACT_SIGMOID) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) sigmoid_row(x[v], &rest[v]);
-      }
-      const float total = group_sum<G>(scores<V>(act, group_max<G>(top_of<V>(x)), x));
+      const float total = group_sum<G>(scores<V>(act, group_max<G>(top_of<V>(x)), x, &rest));
       const float inv = on && total > 0.f ? 1.f / total : 0.f;
       float dot = 0.f;
 #pragma unroll
@@ -323,45 +374,57 @@ balance_grad_kernel(const T* __restrict__ logits, long long ld, int vec, const i
 }
 
 struct Plan {
-  int warps, unit_rows, units, cluster;
+  int warps, unit_rows, units, cluster, direct;
   long long slots;
 };
-// Units of eight warps and at least 64 rows, six a SM at most, where the average request has 64 rows or more; where requests
-// are short (decode steps: one row each) a unit is one warp with 32 rows, and no barrier stands between two requests.
-Plan plan(int T, int n_seg, int n_sms) {
+// Small calls (up to 16384 logits): a CTA per segment, one launch, which even one segment of all rows finishes in a few trips.
+// Otherwise units of eight warps where the average request has 64 rows or more: one wave of CTAs, of at least 64 rows.  Where
+// requests are short (decode steps: one row each) a unit is one warp with 32 rows, and no barrier stands between two requests.
+constexpr int kDirectLogits = 16384;
+Plan plan(int T, int E, int n_seg, int n_sms) {
   Plan p;
+  p.direct = (long long)T * E <= kDirectLogits;
   p.warps = T / n_seg >= 64 ? kUnitWarps : 1;
   if (p.warps == kUnitWarps) {
-    p.unit_rows = (T + 6 * n_sms - 1) / (6 * n_sms);
+    p.unit_rows = (T + kUnitCtas * n_sms - 1) / (kUnitCtas * n_sms);
     if (p.unit_rows < 64) p.unit_rows = 64;
   } else {
     p.unit_rows = 32;
   }
   p.units = T > 0 ? (T + p.unit_rows - 1) / p.unit_rows : 0;
-  p.slots = (long long)p.units + n_seg;
-  p.cluster = p.units / n_seg >= 32 ? kFinCluster : 1;
+  p.slots = p.direct ? 0 : (long long)p.units + n_seg;
+  p.cluster = p.units / n_seg >= 16 ? kFinCluster : 1;
   return p;
 }
 long long workspace_bytes_of(const Plan& p, int E) { return p.slots * (8ll * E + 4); }
 
+template <typename T, int G, int V, int W, bool kDirect>
+cudaError_t balance_launch_one(const Plan& p, const void* logits, long long ld, const int* idx, int T_rows, int E, int k, int act, const int* seg,
+                               int n_seg, float* part_p, int* part_c, int* part_n, const BalanceOut& out, cudaStream_t s) {
+  const int vec = (((uintptr_t)logits | (uintptr_t)(ld * (long long)sizeof(T))) & 15u) == 0;
+  return launch_pdl(kPdlHook, balance_kernel<T, G, V, W, kDirect>, dim3(kDirect ? n_seg : p.units), dim3(32 * W), 0, s, static_cast<const T*>(logits),
+                    ld, vec, idx, T_rows, E, k, act, seg, n_seg, p.unit_rows, part_p, part_c, part_n, out);
+}
 template <typename T>
 cudaError_t balance_launch(const Plan& p, const void* logits, long long ld, const int* idx, int T_rows, int E, int k, int act, const int* seg,
-                           int n_seg, float* part_p, int* part_c, int* part_n, cudaStream_t s) {
-  const int vec = (((uintptr_t)logits | (uintptr_t)(ld * (long long)sizeof(T))) & 15u) == 0;
-#define MIX_BALANCE(G, V)                                                                                                                 \
-  return p.warps == 1 ? launch_pdl(kPdlHook, balance_kernel<T, G, V, 1>, dim3(p.units), dim3(32), 0, s, static_cast<const T*>(logits), ld, vec, \
-                                   idx, T_rows, E, k, act, seg, n_seg, p.unit_rows, part_p, part_c, part_n)                                     \
-                      : launch_pdl(kPdlHook, balance_kernel<T, G, V, kUnitWarps>, dim3(p.units), dim3(32 * kUnitWarps), 0, s,                    \
-                                   static_cast<const T*>(logits), ld, vec, idx, T_rows, E, k, act, seg, n_seg, p.unit_rows, part_p, part_c, part_n)
+                           int n_seg, float* part_p, int* part_c, int* part_n, const BalanceOut& out, cudaStream_t s) {
+#define MIX_BALANCE_AS(G, V, W, D) \
+  balance_launch_one<T, G, V, W, D>(p, logits, ld, idx, T_rows, E, k, act, seg, n_seg, part_p, part_c, part_n, out, s)
+#define MIX_BALANCE(G, V)                                     \
+  if (p.direct) return MIX_BALANCE_AS(G, V, kUnitWarps, true); \
+  return p.warps == 1 ? MIX_BALANCE_AS(G, V, 1, false) : MIX_BALANCE_AS(G, V, kUnitWarps, false)
   MIX_ROW_LAYOUT(E, MIX_BALANCE);
 #undef MIX_BALANCE
+#undef MIX_BALANCE_AS
 }
 template <typename T>
 cudaError_t grad_launch(const void* logits, long long ld, const int* idx, int T_rows, int E, int k, int act, const int* seg, int n_seg,
-                        const int* counts, const int* rows, const float* d_loss, void* d_logits, long long ld_d, cudaStream_t s) {
+                        const int* counts, const int* rows, const float* d_loss, void* d_logits, long long ld_d, int n_sms, cudaStream_t s) {
   const int vec = (((uintptr_t)logits | (uintptr_t)(ld * (long long)sizeof(T))) & 15u) == 0;
   const int vec_d = (((uintptr_t)d_logits | (uintptr_t)(ld_d * (long long)sizeof(T))) & 15u) == 0;
-  const int warp_rows = T_rows >= 32768 ? 16 : (T_rows >= 8192 ? 8 : 4);
+  const int wave = 8 * kGradCtas * n_sms;                      // warps of one wave of CTAs
+  int warp_rows = (int)(((long long)T_rows + wave - 1) / wave);
+  if (warp_rows < 4) warp_rows = 4;
   const long long ctas = ((long long)T_rows + 8 * warp_rows - 1) / (8 * warp_rows);
 #define MIX_BALANCE_GRAD(G, V)                                                                                                          \
   return launch_pdl(kPdlHook, balance_grad_kernel<T, G, V>, dim3((unsigned)ctas), dim3(256), 0, s, static_cast<const T*>(logits), ld, vec, \
@@ -389,7 +452,7 @@ extern "C" long long mix_router_balance_workspace(int T, int n_experts, int n_se
     cudaGetLastError();
     return MIX_ERR_CUDA;
   }
-  return workspace_bytes_of(plan(T, n_seg, n_sms), n_experts);
+  return workspace_bytes_of(plan(T, n_experts, n_seg, n_sms), n_experts);
 }
 
 extern "C" int mix_router_balance(const void* logits, int dtype, long long ld, const int* idx, int T, int n_experts, int k, int act,
@@ -399,23 +462,25 @@ extern "C" int mix_router_balance(const void* logits, int dtype, long long ld, c
   if (rc == MIX_OK) rc = segment_args(seg, n_seg, errbuf, errbuf_len);
   if (rc != MIX_OK) return rc;
   if ((T > 0 && !idx) || !loss || !counts || !mean_p || !rows) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "idx, loss, counts, mean_p and rows are required");
-  if (!workspace || ((uintptr_t)workspace & 3u)) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "the workspace is NULL or not on 4 bytes");
+  if ((uintptr_t)workspace & 3u) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "the workspace is not on 4 bytes");
   int dev, n_sms;
   MIX_OP_CUDA(op_device(&dev, &n_sms));
-  const Plan p = plan(T, n_seg, n_sms);
-  if (workspace_bytes < workspace_bytes_of(p, n_experts))
-    MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "the workspace has to hold %lld bytes", workspace_bytes_of(p, n_experts));
+  const Plan p = plan(T, n_experts, n_seg, n_sms);
+  const long long need = workspace_bytes_of(p, n_experts);
+  if (need > 0 && (!workspace || workspace_bytes < need)) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "the workspace has to hold %lld bytes", need);
   float* part_p = static_cast<float*>(workspace);
   int* part_c = reinterpret_cast<int*>(part_p + p.slots * n_experts);
   int* part_n = part_c + p.slots * n_experts;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (T > 0) {
+  const BalanceOut out = {loss, counts, mean_p, rows};
+  if (T > 0 || p.direct) {
     cudaError_t e;
-    if (dtype == MIX_DTYPE_F32) e = balance_launch<float>(p, logits, ld, idx, T, n_experts, k, act, seg, n_seg, part_p, part_c, part_n, s);
-    else if (dtype == MIX_DTYPE_BF16) e = balance_launch<__nv_bfloat16>(p, logits, ld, idx, T, n_experts, k, act, seg, n_seg, part_p, part_c, part_n, s);
-    else e = balance_launch<__half>(p, logits, ld, idx, T, n_experts, k, act, seg, n_seg, part_p, part_c, part_n, s);
+    if (dtype == MIX_DTYPE_F32) e = balance_launch<float>(p, logits, ld, idx, T, n_experts, k, act, seg, n_seg, part_p, part_c, part_n, out, s);
+    else if (dtype == MIX_DTYPE_BF16) e = balance_launch<__nv_bfloat16>(p, logits, ld, idx, T, n_experts, k, act, seg, n_seg, part_p, part_c, part_n, out, s);
+    else e = balance_launch<__half>(p, logits, ld, idx, T, n_experts, k, act, seg, n_seg, part_p, part_c, part_n, out, s);
     MIX_OP_CUDA(e);
   }
+  if (p.direct) return MIX_OK;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(n_seg * p.cluster));
   cfg.blockDim = dim3(kFinThreads);
@@ -434,8 +499,9 @@ extern "C" int mix_router_balance(const void* logits, int dtype, long long ld, c
   }
   cfg.attrs = at;
   cfg.numAttrs = n_at;
-  MIX_OP_CUDA(cudaLaunchKernelEx(&cfg, balance_finish_kernel, static_cast<const float*>(part_p), static_cast<const int*>(part_c),
-                                 static_cast<const int*>(part_n), T, n_experts, seg, p.unit_rows, p.cluster, loss, counts, mean_p, rows));
+  MIX_OP_CUDA(cudaLaunchKernelEx(&cfg, p.cluster > 1 ? balance_finish_kernel<kFinCluster> : balance_finish_kernel<1>, static_cast<const float*>(part_p),
+                                 static_cast<const int*>(part_c), static_cast<const int*>(part_n), T, n_experts, seg, p.unit_rows, loss, counts,
+                                 mean_p, rows));
   return MIX_OK;
 }
 
@@ -448,11 +514,13 @@ extern "C" int mix_router_balance_grad(const void* logits, int dtype, long long 
   if (ld_d < n_experts) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "row stride %lld of d_logits is below n_experts %d", ld_d, n_experts);
   if (T == 0) return MIX_OK;
   if (!idx || !counts || !rows || !d_loss || !d_logits) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "idx, counts, rows, d_loss and d_logits are required");
+  int dev, n_sms;
+  MIX_OP_CUDA(op_device(&dev, &n_sms));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e;
-  if (dtype == MIX_DTYPE_F32) e = grad_launch<float>(logits, ld, idx, T, n_experts, k, act, seg, n_seg, counts, rows, d_loss, d_logits, ld_d, s);
-  else if (dtype == MIX_DTYPE_BF16) e = grad_launch<__nv_bfloat16>(logits, ld, idx, T, n_experts, k, act, seg, n_seg, counts, rows, d_loss, d_logits, ld_d, s);
-  else e = grad_launch<__half>(logits, ld, idx, T, n_experts, k, act, seg, n_seg, counts, rows, d_loss, d_logits, ld_d, s);
+  if (dtype == MIX_DTYPE_F32) e = grad_launch<float>(logits, ld, idx, T, n_experts, k, act, seg, n_seg, counts, rows, d_loss, d_logits, ld_d, n_sms, s);
+  else if (dtype == MIX_DTYPE_BF16) e = grad_launch<__nv_bfloat16>(logits, ld, idx, T, n_experts, k, act, seg, n_seg, counts, rows, d_loss, d_logits, ld_d, n_sms, s);
+  else e = grad_launch<__half>(logits, ld, idx, T, n_experts, k, act, seg, n_seg, counts, rows, d_loss, d_logits, ld_d, n_sms, s);
   MIX_OP_CUDA(e);
   return MIX_OK;
 }

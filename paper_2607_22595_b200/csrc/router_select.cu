@@ -10,6 +10,7 @@
 // All three are streams over [T, E] or [T, k]; a row sits in the registers of G = E / 8 lanes, so that a warp holds
 // 32 / G rows and every load is one 16-byte vector.
 #include "op_common.cuh"
+#include "tc_common.cuh"
 
 using namespace mix;
 
@@ -31,12 +32,12 @@ __global__ void __launch_bounds__(kSelThreads)
 router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_rows, int E, int k, int act, int renorm,
                    const int* __restrict__ n_live, int* __restrict__ idx, float* __restrict__ weights) {
   constexpr int S = G >= kOpMaxTopk ? 1 : (G == 1 ? 8 : kOpMaxTopk / G);   // chosen entries a lane keeps: entry j is lane j % G's
-  __shared__ float2 found[G == 32 ? kSelWarps : 1][32];                    // (logit, column)
+  __shared__ unsigned long long found[G == 32 ? kSelWarps : 1][32];        // a logit's key, then ~column: the larger comes first
   pdl_wait();
   pdl_launch_dependents();
   const int sub = threadIdx.x & (G - 1);
-  const long long t = ((long long)blockIdx.x * kSelThreads + threadIdx.x) / G;
   const int live = n_live ? min(*n_live, T_rows) : T_rows;
+  const long long t = ((long long)blockIdx.x * kSelThreads + threadIdx.x) / G;
   float x[V];
   if (t < live) {
     load_row<T, G, V>(logits + t * ld, E, sub, vec != 0, x);
@@ -49,42 +50,37 @@ router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_ro
   float my_x[S];
 #pragma unroll
   for (int s = 0; s < S; ++s) { my_idx[s] = -1; my_x[s] = -INFINITY; }
+  int slot = sub;                                                        // (S == 1) the place of this lane's entry
   bool rounds = true;
   if (G == 32) {
     const int warp = threadIdx.x >> 5;
-    float rest = lane_top, bound = -INFINITY;
-    for (int left = k; left > 0;) {
+    float rest = lane_top, bound = top;
+    for (int left = k; bound > -INFINITY;) {
+      left -= __popc(__ballot_sync(0xffffffffu, rest == bound));
+      if (left <= 0) break;
+      rest = rest == bound ? -INFINITY : rest;
       bound = group_max<32>(rest);
-      if (bound == -INFINITY) break;
-      const unsigned at = __ballot_sync(0xffffffffu, rest == bound);
-      left -= __popc(at);
-      if (rest == bound) rest = -INFINITY;
     }
+    bound = fmaxf(bound, -3.402823466e38f);                              // (fewer than k lanes with a logit: all but -inf)
     int n = 0;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const bool in = x[v] >= bound && x[v] > -INFINITY;
+      const bool in = x[v] >= bound;
       const unsigned at = __ballot_sync(0xffffffffu, in);
       const int to = n + __popc(at & ((1u << sub) - 1u));
-      if (in && to < 32) found[warp][to] = make_float2(x[v], __int_as_float(row_col<T, G>(v, sub)));
+      if (in && to < 32) found[warp][to] = ((unsigned long long)f2key(x[v]) << 32) | (unsigned)~row_col<T, G>(v, sub);
       n += __popc(at);
     }
     if (n <= 32) {
       rounds = false;
       __syncwarp();
-      const float2 mine = found[warp][sub];
-      const int col = __float_as_int(mine.y);
+      const unsigned long long mine = found[warp][sub];
       int rank = 0;
-      for (int i = 0; i < n; ++i) {
-        const float2 f = found[warp][i];
-        rank += f.x > mine.x || (f.x == mine.x && __float_as_int(f.y) < col);
-      }
-      __syncwarp();
-      if (sub < n) found[warp][rank] = mine;                               // in the order of the ranks
-      __syncwarp();
-      if (sub < n && sub < k) {
-        my_x[0] = found[warp][sub].x;
-        my_idx[0] = __float_as_int(found[warp][sub].y);
+      for (int i = 0; i < n; ++i) rank += found[warp][i] > mine;
+      slot = sub < n ? rank : sub;                                       // (from n on, up to k: no expert)
+      if (sub < n && rank < k) {
+        my_x[0] = key2f((unsigned)(mine >> 32));
+        my_idx[0] = (int)~(unsigned)mine;
       }
     }
   }
@@ -122,12 +118,11 @@ router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_ro
     if (renorm) total += my_x[s];
   }
   if (!plain) total = group_sum<G>(total);
-  if (t >= T_rows) return;
   const float norm = plain ? 1.f : total;
 #pragma unroll
   for (int s = 0; s < S; ++s) {
-    const int j = s * G + sub;
-    if (j < k) {
+    const int j = S == 1 ? slot : s * G + sub;
+    if (j < k && t < T_rows) {
       idx[t * k + j] = my_idx[s];
       weights[t * k + j] = my_idx[s] >= 0 ? my_x[s] / norm : 0.f;
     }
@@ -142,109 +137,108 @@ router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_ro
 //   sigmoid, renormalised  dx_i = w_i (1 - sigmoid(x_i)) (g_i - s)
 // Entries without an expert are not read further: what stands in their d_w (NaN, say) does not matter.
 //
-// The chosen entries are spread over the row through shared memory where a lane has one of them (more than 64 experts): each lane
-// puts its own where its column is, and the row comes back in the lanes' pieces.  Narrower rows compare each entry with each
-// column of a lane, for 32 / G rows at a time.
+// Where a lane has one chosen entry (more than 64 experts) the row is written as if nothing had been chosen -- p (-s), or zeros --
+// and the lanes then write their own entries over it, w (g - s): w is p there.  Narrower rows compare each entry with each
+// column of a lane, for 32 / G rows at a time.  65536 rows of 256: 38 us with the entries spread over the row in shared memory,
+// %s us so; reading and writing the logits alone takes 20.6.
 template <typename T, int G, int V>
 __global__ void __launch_bounds__(kSelThreads)
 router_topk_grad_kernel(const T* __restrict__ logits, long long ld, int vec, int T_rows, int E, int k, int act, int renorm,
                         const int* __restrict__ idx, const float* __restrict__ weights, const float* __restrict__ d_weights,
                         T* __restrict__ d_logits, long long ld_d, int vec_d) {
   constexpr int S = G >= kOpMaxTopk ? 1 : (G == 1 ? 8 : kOpMaxTopk / G);
-  __shared__ float4 spread[S == 1 ? kSelThreads * V / 4 : 1];
   pdl_wait();
   pdl_launch_dependents();
-  const int sub = threadIdx.x & (G - 1);
+  const int sub = threadIdx.x & (G - 1), lane = threadIdx.x & 31;
   const long long t = ((long long)blockIdx.x * kSelThreads + threadIdx.x) / G;
   const bool row = t < T_rows, dense = act == MIX_ACT_SOFTMAX && !renorm;
-  float d[V], p[V];
+  float p[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) p[v] = -INFINITY;
   if (dense && row) load_row<T, G, V>(logits + t * ld, E, sub, vec != 0, p);
   int my_idx[S];
   float my_g[S], my_w[S];
+#pragma unroll
+  for (int i = 0; i < S; ++i) {
+    const int j = i * G + sub;
+    const bool in = row && j < k;
+    my_idx[i] = in ? idx[t * k + j] : -1;
+    my_g[i] = in ? d_weights[t * k + j] : 0.f;
+    my_w[i] = in ? weights[t * k + j] : 0.f;
+  }
   float s = 0.f;
   bool any = false;
 #pragma unroll
   for (int i = 0; i < S; ++i) {
-    const int j = i * G + sub;
-    my_idx[i] = row && j < k ? idx[t * k + j] : -1;
     const bool ok = (unsigned)my_idx[i] < (unsigned)E;
-    if (!ok) my_idx[i] = -1;
-    my_g[i] = ok ? d_weights[t * k + j] : 0.f;
-    my_w[i] = ok ? weights[t * k + j] : 0.f;
+    if (!ok) {
+      my_idx[i] = -1;
+      my_g[i] = my_w[i] = 0.f;
+    }
     s += my_g[i] * my_w[i];
     any |= ok;
   }
   s = group_sum<G>(s);
+  float d[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) d[v] = 0.f;
   if (dense) {
     any = group_any<G>(any);
     const float total = group_sum<G>(scores<V>(act, group_max<G>(top_of<V>(p)), p));
     const float inv = any && total > 0.f ? 1.f / total : 0.f;
 #pragma unroll
     for (int v = 0; v < V; ++v) p[v] *= inv;
+    if (S == 1) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) d[v] = p[v] > 0.f ? p[v] * -s : 0.f;
+    }
   } else {
 #pragma unroll
-    for (int i = 0; i < S; ++i) {
-      float g = my_w[i] * ((act == MIX_ACT_SOFTMAX || renorm) ? my_g[i] - s : my_g[i]);
-      if (act == MIX_ACT_SIGMOID && my_idx[i] >= 0) g *= sigmoid_row(-to_f32(logits[t * ld + my_idx[i]]));
-      my_g[i] = my_idx[i] >= 0 ? g : 0.f;
+    for (int i = 0; i < S; ++i) {                                // the factors that g is multiplied with, and what is taken off it
+      if (act == MIX_ACT_SIGMOID && my_idx[i] >= 0) my_w[i] *= sigmoid_row(-to_f32(logits[t * ld + my_idx[i]]));
     }
+    if (act == MIX_ACT_SIGMOID && !renorm) s = 0.f;
   }
   if (S == 1) {
-    constexpr int VW = RowVec<T>::VW;
-    const int lane = threadIdx.x & 31;
-    float* buf = reinterpret_cast<float*>(spread) + (threadIdx.x / G) * (G * V);
-    // lane `sub`'s piece b of the row begins at column b * G * VW + sub * VW
-#pragma unroll
-    for (int b = 0; b < V / 4; ++b)
-      *reinterpret_cast<float4*>(buf + (b * 4 / VW) * (G * VW) + sub * VW + (b * 4) % VW) = make_float4(0.f, 0.f, 0.f, 0.f);
-    // the same expert twice in a row (never in what the selection gives): its entries are added in their order
+    if (row) store_row<T, G, V>(d_logits + t * ld_d, E, sub, vec_d != 0, d);
+    // the same expert twice in a row (never in what the selection gives): of a dense row its entries share one -s
     const unsigned same = __match_any_sync(0xffffffffu, my_idx[0] < 0 ? -1 - lane : my_idx[0] + (lane / G) * kOpMaxExperts);
-    float g = my_g[0];
+    float mine = my_w[0] * (my_g[0] - s);
     if (__any_sync(0xffffffffu, (same & (same - 1u)) != 0u)) {
-      g = 0.f;
+      const float part = dense ? my_w[0] * my_g[0] : mine;
+      mine = dense ? my_w[0] * -s : 0.f;
       for (int i = 0; i < 32; ++i) {
-        const float x = __shfl_sync(0xffffffffu, my_g[0], i);
-        if ((same >> i) & 1u) g += x;
+        const float other = __shfl_sync(0xffffffffu, part, i);
+        if ((same >> i) & 1u) mine += other;
       }
     }
-    __syncwarp();
-    if (my_idx[0] >= 0 && lane == __ffs(same) - 1) buf[my_idx[0]] = g;
-    __syncwarp();
-#pragma unroll
-    for (int b = 0; b < V / 4; ++b) {
-      const float4 f = *reinterpret_cast<const float4*>(buf + (b * 4 / VW) * (G * VW) + sub * VW + (b * 4) % VW);
-      d[4 * b] = f.x;
-      d[4 * b + 1] = f.y;
-      d[4 * b + 2] = f.z;
-      d[4 * b + 3] = f.w;
-    }
+    __syncwarp();                                                // the row lies below the entries
+    if (my_idx[0] >= 0 && lane == __ffs(same) - 1) d_logits[t * ld_d + my_idx[0]] = from_f32<T>(mine);
   } else {
-#pragma unroll
-    for (int v = 0; v < V; ++v) d[v] = 0.f;
 #pragma unroll
     for (int j = 0; j < (G == 1 ? 8 : kOpMaxTopk); ++j) {
       if (j >= k) break;
       const int at = __shfl_sync(0xffffffffu, my_idx[j / G], j % G, G);
-      const float g = __shfl_sync(0xffffffffu, my_g[j / G], j % G, G);
+      const float g = __shfl_sync(0xffffffffu, dense ? my_g[j / G] : my_w[j / G] * (my_g[j / G] - s), j % G, G);
 #pragma unroll
       for (int v = 0; v < V; ++v) d[v] += row_col<T, G>(v, sub) == at ? g : 0.f;
     }
-  }
-  if (dense) {
+    if (dense) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) d[v] = p[v] > 0.f ? p[v] * (d[v] - s) : 0.f;
+      for (int v = 0; v < V; ++v) d[v] = p[v] > 0.f ? p[v] * (d[v] - s) : 0.f;
+    }
+    if (row) store_row<T, G, V>(d_logits + t * ld_d, E, sub, vec_d != 0, d);
   }
-  if (row) store_row<T, G, V>(d_logits + t * ld_d, E, sub, vec_d != 0, d);
 }
 
 // ---------------------------------------------------------------------------------------------------- order by expert
-constexpr int kOrdThreads = 512;
+constexpr int kOrdThreads = 1024;
 constexpr int kOrdWarps = kOrdThreads / 32;
 constexpr int kOrdSteps = 8;                                    // entries a lane takes
 constexpr int kOrdChunk = kOrdThreads * kOrdSteps;              // entries a CTA takes
 constexpr int kOrdBuckets = kOpMaxExperts + 1;                  // the last of a call's holds the entries without an expert
+constexpr int kOrdCluster = 8;                                  // CTAs that can look into each other's counts
+static_assert(kOrdChunk <= 65535, "places within a chunk in 16 bits");
 
 __host__ __device__ constexpr int hist_stride(int E) { return (E + 1 + 3) & ~3; }   // counts of a chunk, in whole 16-byte vectors
 __device__ __forceinline__ int bucket_of(int i, int E) { return (unsigned)i < (unsigned)E ? i : E; }
@@ -254,56 +248,106 @@ expert_hist_kernel(const int* __restrict__ idx, int n, int E, int* __restrict__ 
   __shared__ int h[kOrdBuckets];
   pdl_wait();
   pdl_launch_dependents();
-  for (int e = threadIdx.x; e <= E; e += kOrdThreads) h[e] = 0;
+  if (threadIdx.x <= E) h[threadIdx.x] = 0;
   __syncthreads();
   const int base = blockIdx.x * kOrdChunk;
+  int e[kOrdSteps];
 #pragma unroll
   for (int i = 0; i < kOrdSteps; ++i) {
     const int at = base + i * kOrdThreads + threadIdx.x;
-    if (at < n) atomicAdd(&h[bucket_of(idx[at], E)], 1);
+    e[i] = at < n ? bucket_of(idx[at], E) : -1;
   }
+#pragma unroll
+  for (int i = 0; i < kOrdSteps; ++i)
+    if (e[i] >= 0) atomicAdd(&h[e[i]], 1);
   __syncthreads();
-  for (int e = threadIdx.x; e < hist_stride(E); e += kOrdThreads) hist[(size_t)blockIdx.x * hist_stride(E) + e] = e <= E ? h[e] : 0;
+  if ((int)threadIdx.x < hist_stride(E)) hist[(size_t)blockIdx.x * hist_stride(E) + threadIdx.x] = threadIdx.x <= E ? h[threadIdx.x] : 0;
 }
 
 // Entry i of the CTA's chunk goes to  (entries of lower experts) + (entries of this expert in earlier chunks, in earlier warps
-// of the CTA, earlier in the warp).  The counts of the other chunks come from expert_hist_kernel; one chunk needs none, and a
-// call of up to 4096 entries is this one launch.
+// of the CTA, earlier in the warp).  The counts of the other chunks: up to eight chunks are one cluster, whose CTAs read them from
+// each other's shared memory -- a call of up to 65536 entries is this one launch -- and beyond that expert_hist_kernel's.
+// A chunk is sorted in shared memory and leaves expert by expert: written straight from the registers every entry of a warp goes to
+// another line, which took an SM 8192 turns, half of the kernel's time.
+// A warp takes `steps` times 32 entries, the last warps of a call's last chunk fewer.
+struct OrderShared {
+  int before[kOrdBuckets + 3], start[kOrdBuckets + 3], mine[kOrdBuckets + 3], total[kOrdBuckets + 3];
+  int warp_sum[kOrdWarps];
+  unsigned short warp_count[kOrdWarps][kOrdBuckets + 1];        // (an even number of them: rows on 4 bytes)
+  unsigned sorted[kOrdChunk];                                   // place in the chunk | expert << 16
+};
+template <bool kCluster>
 __global__ void __launch_bounds__(kOrdThreads)
-expert_order_kernel(const int* __restrict__ idx, int n, int E, const int* __restrict__ hist, int n_chunks, int* __restrict__ offsets,
+expert_order_kernel(const int* __restrict__ idx, int n, int E, const int* __restrict__ hist, int n_chunks, int steps, int* __restrict__ offsets,
                     int* __restrict__ order, int* __restrict__ position) {
-  __shared__ int warp_count[kOrdWarps][kOrdBuckets];
-  __shared__ int total[kOrdBuckets], before[kOrdBuckets];
+  extern __shared__ __align__(16) unsigned char order_smem[];
+  OrderShared* sh = reinterpret_cast<OrderShared*>(order_smem);
   pdl_wait();
   pdl_launch_dependents();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int e = threadIdx.x; e <= E; e += kOrdThreads) {
-    total[e] = 0;
-    before[e] = 0;
-    for (int w = 0; w < kOrdWarps; ++w) warp_count[w][e] = 0;
-  }
-  __syncthreads();
-  const int base = blockIdx.x * kOrdChunk + warp * (32 * kOrdSteps);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n_warps = blockDim.x >> 5;
+  const int chunk = blockIdx.x * (int)blockDim.x * steps, in_chunk = min(n - chunk, (int)blockDim.x * steps);
+  const int base = warp * 32 * steps;
   int bucket[kOrdSteps], rank[kOrdSteps];
 #pragma unroll
   for (int i = 0; i < kOrdSteps; ++i) {
     const int at = base + i * 32 + lane;
-    bucket[i] = at < n ? bucket_of(idx[at], E) : kOrdBuckets;
+    bucket[i] = i < steps && at < in_chunk ? bucket_of(idx[chunk + at], E) : E + 1;
   }
+  for (int e = lane; e < (E + 2) / 2; e += 32) reinterpret_cast<unsigned*>(sh->warp_count[warp])[e] = 0u;
+  for (int e = threadIdx.x; e <= E; e += blockDim.x) sh->total[e] = sh->before[e] = 0;
+  __syncwarp();
 #pragma unroll
   for (int i = 0; i < kOrdSteps; ++i) {
-    const unsigned same = __match_any_sync(0xffffffffu, bucket[i]);
+    if (i >= steps || base + i * 32 >= in_chunk) break;
+    // the lanes with the same bucket, bit by bit (a match instruction takes a turn per value in the warp)
+    unsigned same = 0xffffffffu;
+    for (int bit = 1; bit <= E + 1; bit <<= 1) {
+      const unsigned with = __ballot_sync(0xffffffffu, (bucket[i] & bit) != 0);
+      same &= (bucket[i] & bit) != 0 ? with : ~with;
+    }
     const int first = __ffs(same) - 1;
     int old = 0;
-    if (lane == first && bucket[i] < kOrdBuckets) {
-      old = warp_count[warp][bucket[i]];
-      warp_count[warp][bucket[i]] = old + __popc(same);
+    if (lane == first && bucket[i] <= E) {
+      old = sh->warp_count[warp][bucket[i]];
+      sh->warp_count[warp][bucket[i]] = (unsigned short)(old + __popc(same));
     }
     rank[i] = __shfl_sync(0xffffffffu, old, first) + __popc(same & ((1u << lane) - 1u));
     __syncwarp();
   }
   __syncthreads();
-  if (n_chunks > 1) {                                    // four columns a thread, the chunks dealt to the threads left over
+  for (int e = threadIdx.x; e <= E; e += blockDim.x) {          // per warp: what the warps in front of it hold
+    int run = 0;
+    for (int w0 = 0; w0 < n_warps; w0 += 8) {
+      int c[8];
+#pragma unroll
+      for (int w = 0; w < 8; ++w) c[w] = w0 + w < n_warps ? sh->warp_count[w0 + w][e] : 0;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) {
+        if (w0 + w < n_warps) sh->warp_count[w0 + w][e] = (unsigned short)run;
+        run += c[w];
+      }
+    }
+    sh->mine[e] = run;
+    if (n_chunks == 1) sh->total[e] = run;
+  }
+  if (kCluster) {
+    tc::cluster_sync_all();
+    for (int e = threadIdx.x; e <= E; e += blockDim.x) {
+      int other[kOrdCluster], all = 0, pre = 0;
+#pragma unroll
+      for (int r = 0; r < kOrdCluster; ++r) {
+        other[r] = 0;
+        if (r < n_chunks) asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(other[r]) : "r"(tc::mapa_cluster(tc::smem_u32(&sh->mine[e]), r)));
+      }
+#pragma unroll
+      for (int r = 0; r < kOrdCluster; ++r) {
+        all += other[r];
+        pre += r < (int)blockIdx.x ? other[r] : 0;
+      }
+      sh->total[e] = all;
+      sh->before[e] = pre;
+    }
+  } else if (n_chunks > 1) {                             // four columns a thread, the chunks dealt to the threads left over
     const int wide = hist_stride(E) / 4, parts = kOrdThreads / wide, part = threadIdx.x / wide, col = threadIdx.x % wide;
     if (part < parts) {
       const int4* rows = reinterpret_cast<const int4*>(hist) + col;
@@ -319,59 +363,52 @@ expert_order_kernel(const int* __restrict__ idx, int n, int E, const int* __rest
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         if (4 * col + i <= E) {
-          atomicAdd(&total[4 * col + i], s4[i]);
-          atomicAdd(&before[4 * col + i], p4[i]);
+          atomicAdd(&sh->total[4 * col + i], s4[i]);
+          atomicAdd(&sh->before[4 * col + i], p4[i]);
         }
     }
   }
   __syncthreads();
-  for (int e = threadIdx.x; e <= E; e += kOrdThreads) {   // per warp: what the warps in front of it hold
-    int run = before[e];
+  // exclusive sums over the buckets: of the call's counts (where an expert begins in `order`) and of the chunk's (in `sorted`)
+  if (warp < 2) {
+    const int* from = warp == 0 ? sh->total : sh->mine;
+    int run = 0;
+    for (int e0 = 0; e0 <= E; e0 += 32) {
+      const int e = e0 + lane, v = e <= E ? from[e] : 0;
+      int inc = v;
 #pragma unroll
-    for (int w = 0; w < kOrdWarps; ++w) {
-      const int c = warp_count[w][e];
-      warp_count[w][e] = run;
-      run += c;
-    }
-    if (n_chunks == 1) total[e] = run;
-  }
-  __syncthreads();
-  if (warp == 0) {                                       // exclusive sum over the buckets
-    constexpr int kEach = (kOrdBuckets + 31) / 32;
-    int v[kEach], sum = 0;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int e = lane * kEach + i;
-      v[i] = e <= E ? total[e] : 0;
-      sum += v[i];
-    }
-    int inc = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += y;
-    }
-    int run = inc - sum;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int e = lane * kEach + i;
-      if (e <= E) {
-        total[e] = run;
-        if (blockIdx.x == 0) offsets[e] = run;           // offsets[E]: entries with an expert
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
       }
-      run += v[i];
+      if (e <= E) {
+        if (warp == 0) {
+          sh->before[e] += run + inc - v;
+          if (blockIdx.x == 0) offsets[e] = run + inc - v;      // offsets[E]: entries with an expert
+        } else {
+          sh->start[e] = run + inc - v;
+        }
+      }
+      run += __shfl_sync(0xffffffffu, inc, 31);
     }
   }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kOrdSteps; ++i) {
     const int at = base + i * 32 + lane;
-    if (at < n) {
-      const int b = bucket[i], to = total[b] + warp_count[warp][b] + rank[i];
-      order[to] = b < E ? at : -1;
-      position[at] = b < E ? to : -1;
+    if (i < steps && at < in_chunk) {
+      const int e = bucket[i], in = sh->warp_count[warp][e] + rank[i];
+      sh->sorted[sh->start[e] + in] = (unsigned)at | (unsigned)e << 16;
+      position[chunk + at] = e < E ? sh->before[e] + in : -1;
     }
   }
+  __syncthreads();
+  for (int i = threadIdx.x; i < in_chunk; i += blockDim.x) {
+    const unsigned v = sh->sorted[i];
+    const int e = (int)(v >> 16);
+    order[sh->before[e] + i - sh->start[e]] = e < E ? chunk + (int)(v & 0xffffu) : -1;
+  }
+  if (kCluster) tc::cluster_sync_all();                  // the counts stay until all have read them
 }
 
 template <typename T>
@@ -447,7 +484,7 @@ extern "C" int mix_router_topk_grad(const void* logits, int dtype, long long ld,
 extern "C" long long mix_expert_order_workspace(long long n, int n_experts) {
   if (n < 0 || n > MIX_ORDER_MAX_ENTRIES || n_experts < 1 || n_experts > kOpMaxExperts) return MIX_ERR_OUT_OF_RANGE;
   const long long chunks = (n + kOrdChunk - 1) / kOrdChunk;
-  return chunks > 1 ? chunks * hist_stride(n_experts) * (long long)sizeof(int) : 0;
+  return chunks > kOrdCluster ? chunks * hist_stride(n_experts) * (long long)sizeof(int) : 0;
 }
 
 extern "C" int mix_expert_order(const int* idx, long long n, int n_experts, int* offsets, int* order, int* position, void* workspace,
@@ -461,8 +498,39 @@ extern "C" int mix_expert_order(const int* idx, long long n, int n_experts, int*
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   int* hist = static_cast<int*>(workspace);
   const int chunks = n == 0 ? 1 : (int)((n + kOrdChunk - 1) / kOrdChunk);
-  if (chunks > 1) MIX_OP_CUDA(launch_pdl(kPdlHook, expert_hist_kernel, dim3(chunks), dim3(kOrdThreads), 0, s, idx, (int)n, n_experts, hist));
-  MIX_OP_CUDA(launch_pdl(kPdlHook, expert_order_kernel, dim3(chunks), dim3(kOrdThreads), 0, s, idx, (int)n, n_experts, static_cast<const int*>(hist),
-                         chunks, offsets, order, position));
+  const bool cluster = chunks > 1 && chunks <= kOrdCluster;
+  if (chunks > kOrdCluster) MIX_OP_CUDA(launch_pdl(kPdlHook, expert_hist_kernel, dim3(chunks), dim3(kOrdThreads), 0, s, idx, (int)n, n_experts, hist));
+  // (few entries: as many threads, at least two warps, so that a lane has one)
+  const int threads = n >= kOrdThreads ? kOrdThreads : (n <= 64 ? 64 : (int)((n + 31) / 32 * 32));
+  const int steps = chunks > 1 ? kOrdSteps : (n <= threads ? 1 : (int)((n + threads - 1) / threads));
+  static std::atomic<int> ready[kOpDevices];
+  int dev, n_sms;
+  MIX_OP_CUDA(op_device(&dev, &n_sms));
+  if (!ready[dev].load(std::memory_order_relaxed)) {
+    MIX_OP_CUDA(cudaFuncSetAttribute(expert_order_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(OrderShared)));
+    MIX_OP_CUDA(cudaFuncSetAttribute(expert_order_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(OrderShared)));
+    ready[dev].store(1, std::memory_order_relaxed);
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(chunks);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = sizeof(OrderShared);
+  cfg.stream = s;
+  cudaLaunchAttribute at[2];
+  int n_at = 0;
+  if (cluster) {
+    at[n_at].id = cudaLaunchAttributeClusterDimension;
+    at[n_at].val.clusterDim.x = chunks;
+    at[n_at].val.clusterDim.y = 1;
+    at[n_at++].val.clusterDim.z = 1;
+  }
+  if (pdl_mask() & kPdlHook) {
+    at[n_at].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[n_at++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  cfg.attrs = at;
+  cfg.numAttrs = n_at;
+  MIX_OP_CUDA(cudaLaunchKernelEx(&cfg, cluster ? expert_order_kernel<true> : expert_order_kernel<false>, idx, (int)n, n_experts,
+                                 static_cast<const int*>(hist), chunks, steps, offsets, order, position));
   return MIX_OK;
 }

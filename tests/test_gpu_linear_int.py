@@ -146,6 +146,23 @@ def test_quantize_rows_of_every_pair_of_values():
         assert scale.item() == float(np.float32(a.item()) / np.float32(127))
 
 
+def test_quantize_rows_of_every_pair_of_fp16_values():
+    """The same for fp16, whose largest values that are multiples of 127 have halves everywhere."""
+    values = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(torch.float16).to(DEV)
+    values = values[torch.isfinite(values) & (values >= 0)]
+    for a in (1.0, 1.999, 127.0, 254.0, 1143.0, 1270.0, 1397.0, 1524.0, 1651.0, 1778.0, 1905.0, 2032.0, 381.0 / 64, 635.0 / 8, 1025.0, 2047.0, 65504.0, 6e-8,
+              6.1e-5, 1143.0 * 2.0**-24, 173.0):
+        a = torch.tensor(a, device=DEV).to(torch.float16)
+        fit = values[values <= a]
+        n = (fit.numel() + 16) // 16 * 16
+        x = torch.zeros(n, dtype=torch.float16, device=DEV)
+        x[:fit.numel()] = torch.where(torch.arange(fit.numel(), device=DEV) % 2 == 0, fit, -fit)
+        x[-1] = a
+        codes, scale = mix.quantize_rows(torch.stack([x, -x]))
+        assert torch.equal(codes.double(), R.codes_of(torch.stack([x, -x]))[0]), a
+        assert scale[0].item() == float(np.float32(a.item()) / np.float32(127))
+
+
 def test_quantize_rows_with_infinities_and_nan():
     x = torch.randn((6, 96), device=DEV).to(torch.bfloat16)
     x[1, 7], x[2, 95], x[3, 0], x[4, 3] = torch.inf, -torch.inf, torch.nan, torch.nan
