@@ -546,7 +546,7 @@ int mix_router_topk_grad(const void* logits, int dtype, long long ld, int T, int
    those of expert 1, and so on, each expert's in rising order; -1 behind them.  offsets int32 [n_experts + 1]: expert e's are
    order[offsets[e] .. offsets[e + 1]), so differences of neighbours are the per-expert counts.  position int32 [n]: the place of an entry in
    `order`, -1 for entries that name no expert (idx outside [0, n_experts)).
-   workspace: mix_expert_order_workspace(n, n_experts) bytes (0 for up to 65536 entries; negative: a mix_status), on 16 bytes.
+   workspace: mix_expert_order_workspace(n, n_experts) bytes (0 for up to 16384 entries; negative: a mix_status), on 16 bytes.
    Errors: OUT_OF_RANGE (n outside [0, MIX_ORDER_MAX_ENTRIES], n_experts), INVALID_ARG. */
 long long mix_expert_order_workspace(long long n, int n_experts);
 int mix_expert_order(const int* idx, long long n, int n_experts, int* offsets, int* order, int* position, void* workspace,

@@ -72,7 +72,7 @@ __device__ __noinline__ uint2 codes8_divided(const uint4& raw, float a) {
 
 constexpr int kQuantVecs = 4;                                  // 8-element vectors a thread keeps
 template <typename T, int THREADS, bool vec>
-__global__ void __launch_bounds__(THREADS < 128 ? 128 : THREADS, THREADS == 256 ? 6 : 12)
+__global__ void __launch_bounds__(THREADS < 128 ? 128 : THREADS, THREADS == 256 ? 6 : (THREADS == 128 ? 12 : 9))
 quantize_rows_kernel(const T* __restrict__ x, long long ld, int x_rows, const int* __restrict__ order, int div, int n_rows, int d,
                      signed char* __restrict__ codes, float* __restrict__ scale) {
   constexpr int kRows = THREADS < 128 ? 128 / THREADS : 1;     // rows a CTA takes

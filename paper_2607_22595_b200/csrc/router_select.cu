@@ -22,17 +22,18 @@ constexpr int kSelThreads = 256;
 // The selection compares the logits themselves, never probabilities: those round, and two logits that differ could tie.
 //
 // Rows of up to 128 experts: k rounds of an arg-max over the G lanes, 32 / G rows of a warp side by side.
-// Wider rows (a warp each): the k-th largest of the lanes' own largest logits is a lower bound on the row's k-th largest logit,
-// and only a few more than k logits reach it.  Those go to shared memory, one to a lane, and each counts how many come before it.
-// Where more than 32 reach it (many equal logits) the rounds decide.  65536 rows of 256, k = 8, with the softmax over the row:
-// 76 us by rounds, %s us so; the logits' stream alone takes 10.3.
-constexpr int kSelWarps = kSelThreads / 32;
+// Wider rows (a warp each) are bound by comparisons and selections, which issue at half rate, so they compare keys that carry the
+// column: the logit's order-preserving bits, the lowest 8 or 9 replaced by ~column.  No two are equal, a round is one reduction
+// over the warp, and a lane keeps its two largest keys; one that has given its first offers its second.  k + 1 rounds.  The row
+// is done again by rounds over all logits where that may not be the answer: a lane gave both and has more above the last key
+// (8 of 256: a row in twenty), or two neighbours of fp32 agree in all bits of the key (16-bit logits lose none).
+// 65536 rows of 256, k = 8, with the softmax over the row: 76 us by rounds over all logits, 37 with logits and columns apart, %s us
+// so; the logits' stream alone takes 10.3.
 template <typename T, int G, int V>
 __global__ void __launch_bounds__(kSelThreads)
 router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_rows, int E, int k, int act, int renorm,
                    const int* __restrict__ n_live, int* __restrict__ idx, float* __restrict__ weights) {
   constexpr int S = G >= kOpMaxTopk ? 1 : (G == 1 ? 8 : kOpMaxTopk / G);   // chosen entries a lane keeps: entry j is lane j % G's
-  __shared__ unsigned long long found[G == 32 ? kSelWarps : 1][32];        // a logit's key, then ~column: the larger comes first
   pdl_wait();
   pdl_launch_dependents();
   const int sub = threadIdx.x & (G - 1);
@@ -50,38 +51,56 @@ router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_ro
   float my_x[S];
 #pragma unroll
   for (int s = 0; s < S; ++s) { my_idx[s] = -1; my_x[s] = -INFINITY; }
-  int slot = sub;                                                        // (S == 1) the place of this lane's entry
   bool rounds = true;
   if (G == 32) {
-    const int warp = threadIdx.x >> 5;
-    float rest = lane_top, bound = top;
-    for (int left = k; bound > -INFINITY;) {
-      left -= __popc(__ballot_sync(0xffffffffu, rest == bound));
-      if (left <= 0) break;
-      rest = rest == bound ? -INFINITY : rest;
-      bound = group_max<32>(rest);
-    }
-    bound = fmaxf(bound, -3.402823466e38f);                              // (fewer than k lanes with a logit: all but -inf)
-    int n = 0;
+    constexpr unsigned kCol = V * 32 - 1;                                  // the key's bits that hold ~column
+    constexpr unsigned kNone = 0x007fffffu & ~kCol;                        // -inf's key
+    static_assert((kCol & V * 32) == 0, "a power of two");
+    unsigned key[V], hi[V / 2], lo[V / 2];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const bool in = x[v] >= bound;
-      const unsigned at = __ballot_sync(0xffffffffu, in);
-      const int to = n + __popc(at & ((1u << sub) - 1u));
-      if (in && to < 32) found[warp][to] = ((unsigned long long)f2key(x[v]) << 32) | (unsigned)~row_col<T, G>(v, sub);
-      n += __popc(at);
+      const unsigned bits = __float_as_uint(x[v] + 0.f);                   // -0 and 0 are equal
+      key[v] = ((bits ^ ((unsigned)((int)bits >> 31) | 0x80000000u)) & ~kCol) | (kCol - (unsigned)row_col<T, G>(v, sub));
     }
-    if (n <= 32) {
-      rounds = false;
-      __syncwarp();
-      const unsigned long long mine = found[warp][sub];
-      int rank = 0;
-      for (int i = 0; i < n; ++i) rank += found[warp][i] > mine;
-      slot = sub < n ? rank : sub;                                       // (from n on, up to k: no expert)
-      if (sub < n && rank < k) {
-        my_x[0] = key2f((unsigned)(mine >> 32));
-        my_idx[0] = (int)~(unsigned)mine;
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+      hi[i] = max(key[2 * i], key[2 * i + 1]);
+      lo[i] = min(key[2 * i], key[2 * i + 1]);
+    }
+#pragma unroll
+    for (int n = V / 4; n > 0; n /= 2) {
+#pragma unroll
+      for (int i = 0; i < n; ++i) {
+        lo[i] = max(min(hi[i], hi[i + n]), max(lo[i], lo[i + n]));
+        hi[i] = max(hi[i], hi[i + n]);
       }
+    }
+    unsigned first = hi[0], second = lo[0], last = 0u, mine = 0u;
+    int given = 0;
+#pragma unroll
+    for (int j = 0; j < kOpMaxTopk + 1; ++j) {
+      if (j > k) break;
+      last = __reduce_max_sync(0xffffffffu, first);
+      if ((last & ~kCol) <= kNone) break;                                  // nothing but -inf on offer
+      mine = j == sub ? last : mine;
+      if (first == last) {
+        first = second;
+        second = 0u;
+        ++given;
+      }
+    }
+    last = max(last, kNone + kCol + 1u);
+    int above = 0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) above += key[v] >= last;
+    const unsigned after = __shfl_down_sync(0xffffffffu, mine, 1);         // (by all lanes)
+    bool unsure = above != given;
+    if (sizeof(T) == 4) unsure |= sub < k && mine != 0u && ((after ^ mine) & ~kCol) == 0u;
+    rounds = __any_sync(0xffffffffu, unsure);
+    if (!rounds && sub < k && mine != 0u) {
+      my_idx[0] = (int)(kCol - (mine & kCol));
+      // (the bits that gave way to the column were 0 in a 16-bit logit, 1 in the key of a negative one)
+      my_x[0] = sizeof(T) == 4 ? to_f32(logits[t * ld + my_idx[0]]) : key2f((mine & 0x80000000u) ? mine & ~kCol : mine | kCol);
     }
   }
   if (rounds) {
@@ -121,7 +140,7 @@ router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_ro
   const float norm = plain ? 1.f : total;
 #pragma unroll
   for (int s = 0; s < S; ++s) {
-    const int j = S == 1 ? slot : s * G + sub;
+    const int j = s * G + sub;
     if (j < k && t < T_rows) {
       idx[t * k + j] = my_idx[s];
       weights[t * k + j] = my_idx[s] >= 0 ? my_x[s] / norm : 0.f;
@@ -186,11 +205,11 @@ router_topk_grad_kernel(const T* __restrict__ logits, long long ld, int vec, int
     any = group_any<G>(any);
     const float total = group_sum<G>(scores<V>(act, group_max<G>(top_of<V>(p)), p));
     const float inv = any && total > 0.f ? 1.f / total : 0.f;
+    const float less = S == 1 ? inv * -s : inv;
 #pragma unroll
-    for (int v = 0; v < V; ++v) p[v] *= inv;
-    if (S == 1) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) d[v] = p[v] > 0.f ? p[v] * -s : 0.f;
+    for (int v = 0; v < V; ++v) {
+      p[v] *= less;
+      if (S == 1) d[v] = p[v];
     }
   } else {
 #pragma unroll
@@ -202,9 +221,9 @@ router_topk_grad_kernel(const T* __restrict__ logits, long long ld, int vec, int
   if (S == 1) {
     if (row) store_row<T, G, V>(d_logits + t * ld_d, E, sub, vec_d != 0, d);
     // the same expert twice in a row (never in what the selection gives): of a dense row its entries share one -s
-    const unsigned same = __match_any_sync(0xffffffffu, my_idx[0] < 0 ? -1 - lane : my_idx[0] + (lane / G) * kOpMaxExperts);
+    const unsigned same = __match_any_sync(0xffffffffu, my_idx[0] < 0 ? -1 : my_idx[0] + (lane / G) * kOpMaxExperts);
     float mine = my_w[0] * (my_g[0] - s);
-    if (__any_sync(0xffffffffu, (same & (same - 1u)) != 0u)) {
+    if (__any_sync(0xffffffffu, my_idx[0] >= 0 && (same & (same - 1u)) != 0u)) {
       const float part = dense ? my_w[0] * my_g[0] : mine;
       mine = dense ? my_w[0] * -s : 0.f;
       for (int i = 0; i < 32; ++i) {
@@ -225,7 +244,7 @@ router_topk_grad_kernel(const T* __restrict__ logits, long long ld, int vec, int
     }
     if (dense) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) d[v] = p[v] > 0.f ? p[v] * (d[v] - s) : 0.f;
+      for (int v = 0; v < V; ++v) d[v] = p[v] * (d[v] - s);
     }
     if (row) store_row<T, G, V>(d_logits + t * ld_d, E, sub, vec_d != 0, d);
   }
@@ -235,7 +254,7 @@ router_topk_grad_kernel(const T* __restrict__ logits, long long ld, int vec, int
 constexpr int kOrdThreads = 1024;
 constexpr int kOrdWarps = kOrdThreads / 32;
 constexpr int kOrdSteps = 8;                                    // entries a lane takes
-constexpr int kOrdChunk = kOrdThreads * kOrdSteps;              // entries a CTA takes
+constexpr int kOrdChunk = kOrdThreads * kOrdSteps;              // entries a CTA takes, at most
 constexpr int kOrdBuckets = kOpMaxExperts + 1;                  // the last of a call's holds the entries without an expert
 constexpr int kOrdCluster = 8;                                  // CTAs that can look into each other's counts
 static_assert(kOrdChunk <= 65535, "places within a chunk in 16 bits");
@@ -244,29 +263,29 @@ __host__ __device__ constexpr int hist_stride(int E) { return (E + 1 + 3) & ~3; 
 __device__ __forceinline__ int bucket_of(int i, int E) { return (unsigned)i < (unsigned)E ? i : E; }
 
 __global__ void __launch_bounds__(kOrdThreads)
-expert_hist_kernel(const int* __restrict__ idx, int n, int E, int* __restrict__ hist) {
+expert_hist_kernel(const int* __restrict__ idx, int n, int E, int steps, int* __restrict__ hist) {
   __shared__ int h[kOrdBuckets];
   pdl_wait();
   pdl_launch_dependents();
-  if (threadIdx.x <= E) h[threadIdx.x] = 0;
-  __syncthreads();
-  const int base = blockIdx.x * kOrdChunk;
+  const int threads = blockDim.x, base = blockIdx.x * threads * steps;
   int e[kOrdSteps];
 #pragma unroll
   for (int i = 0; i < kOrdSteps; ++i) {
-    const int at = base + i * kOrdThreads + threadIdx.x;
-    e[i] = at < n ? bucket_of(idx[at], E) : -1;
+    const int at = base + i * threads + threadIdx.x;
+    e[i] = i < steps && at < n ? bucket_of(idx[at], E) : -1;
   }
+  for (int i = threadIdx.x; i <= E; i += threads) h[i] = 0;
+  __syncthreads();
 #pragma unroll
   for (int i = 0; i < kOrdSteps; ++i)
     if (e[i] >= 0) atomicAdd(&h[e[i]], 1);
   __syncthreads();
-  if ((int)threadIdx.x < hist_stride(E)) hist[(size_t)blockIdx.x * hist_stride(E) + threadIdx.x] = threadIdx.x <= E ? h[threadIdx.x] : 0;
+  for (int i = threadIdx.x; i < hist_stride(E); i += threads) hist[(size_t)blockIdx.x * hist_stride(E) + i] = i <= E ? h[i] : 0;
 }
 
 // Entry i of the CTA's chunk goes to  (entries of lower experts) + (entries of this expert in earlier chunks, in earlier warps
 // of the CTA, earlier in the warp).  The counts of the other chunks: up to eight chunks are one cluster, whose CTAs read them from
-// each other's shared memory -- a call of up to 65536 entries is this one launch -- and beyond that expert_hist_kernel's.
+// each other's shared memory -- a call of up to 16384 entries is this one launch -- and beyond that expert_hist_kernel's.
 // A chunk is sorted in shared memory and leaves expert by expert: written straight from the registers every entry of a warp goes to
 // another line, which took an SM 8192 turns, half of the kernel's time.
 // A warp takes `steps` times 32 entries, the last warps of a call's last chunk fewer.
@@ -348,7 +367,7 @@ expert_order_kernel(const int* __restrict__ idx, int n, int E, const int* __rest
       sh->before[e] = pre;
     }
   } else if (n_chunks > 1) {                             // four columns a thread, the chunks dealt to the threads left over
-    const int wide = hist_stride(E) / 4, parts = kOrdThreads / wide, part = threadIdx.x / wide, col = threadIdx.x % wide;
+    const int wide = hist_stride(E) / 4, parts = (int)blockDim.x / wide, part = threadIdx.x / wide, col = threadIdx.x % wide;
     if (part < parts) {
       const int4* rows = reinterpret_cast<const int4*>(hist) + col;
       int4 sum = make_int4(0, 0, 0, 0), pre = make_int4(0, 0, 0, 0);
@@ -481,10 +500,40 @@ extern "C" int mix_router_topk_grad(const void* logits, int dtype, long long ld,
   return MIX_OK;
 }
 
+namespace {
+// How a call's entries are dealt.  What a step of a warp costs is instructions, some 90, so a chunk is small and many SMs share the
+// work: 16384 entries on 8 SMs of 512 threads, beyond that chunks of 2048 or 4096 entries as long as there are no more than 64 of
+// them -- every CTA reads all chunks' counts.  (65536 entries of 256 experts: %s us, 12.5 in eight chunks of 8192; 16384: %s, 12.3 in two.)
+struct OrderPlan {
+  int threads, steps, chunks;
+  bool cluster, counts;
+};
+OrderPlan order_plan(long long n) {
+  OrderPlan p = {kOrdThreads, kOrdSteps, 1, false, false};
+  const auto chunks = [&](int threads, int steps) { return (int)((n + threads * steps - 1) / (threads * steps)); };
+  if (n <= 512) {
+    p.threads = n <= 64 ? 64 : (int)((n + 31) / 32 * 32);
+    p.steps = 1;
+  } else if (n <= 8 * 2048) {                                  // one cluster, 512 entries or more a CTA
+    p.chunks = n <= 1024 ? 2 : (n <= 2048 ? 4 : kOrdCluster);
+    p.threads = n <= 4096 ? 256 : 512;
+    p.steps = (int)((n + (long long)p.threads * p.chunks - 1) / ((long long)p.threads * p.chunks));
+    p.chunks = chunks(p.threads, p.steps);
+    p.cluster = p.chunks > 1;
+  } else {
+    if (chunks(512, 4) <= 64) { p.threads = 512; p.steps = 4; }
+    else if (chunks(512, 8) <= 64) { p.threads = 512; }
+    p.chunks = chunks(p.threads, p.steps);
+    p.counts = true;
+  }
+  return p;
+}
+}  // namespace
+
 extern "C" long long mix_expert_order_workspace(long long n, int n_experts) {
   if (n < 0 || n > MIX_ORDER_MAX_ENTRIES || n_experts < 1 || n_experts > kOpMaxExperts) return MIX_ERR_OUT_OF_RANGE;
-  const long long chunks = (n + kOrdChunk - 1) / kOrdChunk;
-  return chunks > kOrdCluster ? chunks * hist_stride(n_experts) * (long long)sizeof(int) : 0;
+  const OrderPlan p = order_plan(n);
+  return p.counts ? (long long)p.chunks * hist_stride(n_experts) * (long long)sizeof(int) : 0;
 }
 
 extern "C" int mix_expert_order(const int* idx, long long n, int n_experts, int* offsets, int* order, int* position, void* workspace,
@@ -497,12 +546,7 @@ extern "C" int mix_expert_order(const int* idx, long long n, int n_experts, int*
     MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "the workspace has to hold %lld bytes, on 16 bytes", need);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   int* hist = static_cast<int*>(workspace);
-  const int chunks = n == 0 ? 1 : (int)((n + kOrdChunk - 1) / kOrdChunk);
-  const bool cluster = chunks > 1 && chunks <= kOrdCluster;
-  if (chunks > kOrdCluster) MIX_OP_CUDA(launch_pdl(kPdlHook, expert_hist_kernel, dim3(chunks), dim3(kOrdThreads), 0, s, idx, (int)n, n_experts, hist));
-  // (few entries: as many threads, at least two warps, so that a lane has one)
-  const int threads = n >= kOrdThreads ? kOrdThreads : (n <= 64 ? 64 : (int)((n + 31) / 32 * 32));
-  const int steps = chunks > 1 ? kOrdSteps : (n <= threads ? 1 : (int)((n + threads - 1) / threads));
+  const OrderPlan p = order_plan(n);
   static std::atomic<int> ready[kOpDevices];
   int dev, n_sms;
   MIX_OP_CUDA(op_device(&dev, &n_sms));
@@ -511,16 +555,17 @@ extern "C" int mix_expert_order(const int* idx, long long n, int n_experts, int*
     MIX_OP_CUDA(cudaFuncSetAttribute(expert_order_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(OrderShared)));
     ready[dev].store(1, std::memory_order_relaxed);
   }
+  if (p.counts) MIX_OP_CUDA(launch_pdl(kPdlHook, expert_hist_kernel, dim3(p.chunks), dim3(p.threads), 0, s, idx, (int)n, n_experts, p.steps, hist));
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(chunks);
-  cfg.blockDim = dim3(threads);
+  cfg.gridDim = dim3(p.chunks);
+  cfg.blockDim = dim3(p.threads);
   cfg.dynamicSmemBytes = sizeof(OrderShared);
   cfg.stream = s;
   cudaLaunchAttribute at[2];
   int n_at = 0;
-  if (cluster) {
+  if (p.cluster) {
     at[n_at].id = cudaLaunchAttributeClusterDimension;
-    at[n_at].val.clusterDim.x = chunks;
+    at[n_at].val.clusterDim.x = p.chunks;
     at[n_at].val.clusterDim.y = 1;
     at[n_at++].val.clusterDim.z = 1;
   }
@@ -530,7 +575,7 @@ extern "C" int mix_expert_order(const int* idx, long long n, int n_experts, int*
   }
   cfg.attrs = at;
   cfg.numAttrs = n_at;
-  MIX_OP_CUDA(cudaLaunchKernelEx(&cfg, cluster ? expert_order_kernel<true> : expert_order_kernel<false>, idx, (int)n, n_experts,
-                                 static_cast<const int*>(hist), chunks, steps, offsets, order, position));
+  MIX_OP_CUDA(cudaLaunchKernelEx(&cfg, p.cluster ? expert_order_kernel<true> : expert_order_kernel<false>, idx, (int)n, n_experts,
+                                 static_cast<const int*>(hist), p.chunks, p.steps, offsets, order, position));
   return MIX_OK;
 }

@@ -126,7 +126,7 @@ def test_the_same_expert_twice_in_a_row():
     assert counts[0].tolist() == [0, 0, 0, 18, 0, 0, 0, 0] and rows.tolist() == [9]
 
 
-ORDERS = [(0, 2, 8), (1, 1, 1), (1, 2, 8), (64, 2, 8), (100, 6, 64), (511, 8, 33), (512, 8, 256), (513, 8, 512), (1000, 5, 7), (3000, 8, 100), (4096, 2, 9), (4097, 2, 3), (5000, 16, 511), (4096, 16, 64), (4097, 16, 64), (20000, 6, 100)]
+ORDERS = [(0, 2, 8), (1, 1, 1), (1, 2, 8), (64, 2, 8), (100, 6, 64), (511, 8, 33), (512, 8, 256), (513, 8, 512), (1000, 5, 7), (3000, 8, 100), (4096, 2, 9), (4097, 2, 3), (5000, 16, 511), (4096, 16, 64), (4097, 16, 64), (20000, 6, 100), (1024, 1, 5), (1025, 1, 5), (2050, 1, 300), (8192, 2, 8), (8193, 2, 8), (41000, 8, 12), (90000, 8, 7), (100000, 14, 4)]
 
 
 @pytest.mark.parametrize("T,k,E", ORDERS)

@@ -22,7 +22,7 @@ REFUSED = [
     ("topk", {9: None}, INVALID), ("topk", {10: None}, INVALID),
     ("topk_grad", {0: None}, INVALID), ("topk_grad", {12: 7}, RANGE), ("topk_grad", {11: None}, INVALID), ("topk_grad", {8: None}, INVALID),
     ("order", {0: None}, INVALID), ("order", {1: -1}, RANGE), ("order", {1: (1 << 24) + 1}, RANGE), ("order", {2: 0}, RANGE), ("order", {2: 513}, RANGE),
-    ("order", {3: None}, INVALID), ("order", {1: 65537}, INVALID), ("order", {1: 65537, 6: P, 7: 8}, INVALID), ("order", {1: 65537, 6: P + 4, 7: 4096}, INVALID),
+    ("order", {3: None}, INVALID), ("order", {1: 16385}, INVALID), ("order", {1: 16385, 6: P, 7: 8}, INVALID), ("order", {1: 16385, 6: P + 4, 7: 1 << 20}, INVALID),
     ("balance", {0: None}, INVALID), ("balance", {3: None}, INVALID), ("balance", {9: 0}, RANGE), ("balance", {9: 65537}, RANGE), ("balance", {9: 2}, INVALID),
     ("balance", {10: None}, INVALID), ("balance", {14: P + 1}, INVALID), ("balance", {6: 9}, RANGE),
     ("balance_grad", {14: 7}, RANGE), ("balance_grad", {10: None}, INVALID), ("balance_grad", {8: P, 9: 0}, RANGE),
@@ -52,8 +52,8 @@ def test_refused_with_a_message(which, change, code):
 
 def test_workspace_sizes():
     lib = mix.load_library()
-    assert lib.mix_expert_order_workspace(0, 8) == 0 and lib.mix_expert_order_workspace(65536, 8) == 0
-    assert lib.mix_expert_order_workspace(65537, 8) >= 9 * 9 * 4
+    assert lib.mix_expert_order_workspace(0, 8) == 0 and lib.mix_expert_order_workspace(16384, 8) == 0
+    assert lib.mix_expert_order_workspace(16385, 8) >= 9 * 9 * 4
     assert lib.mix_expert_order_workspace(1 << 24, 512) > 0
     assert lib.mix_expert_order_workspace((1 << 24) + 1, 8) < 0 and lib.mix_expert_order_workspace(5, 0) < 0
     assert lib.mix_router_balance_workspace(-1, 8, 1) == RANGE and lib.mix_router_balance_workspace(4, 513, 1) == RANGE
