@@ -75,7 +75,7 @@ __device__ __forceinline__ int row_col(int v, int sub) {
   constexpr int VW = RowVec<T>::VW;
   return (v / VW) * (G * VW) + sub * VW + v % VW;
 }
-// Columns behind the row's end and NaN read as -inf: no probability, never chosen.
+// Columns behind the row's end read as -inf: no probability, never chosen.
 template <typename T, int G, int V>
 __device__ __forceinline__ void load_row(const T* __restrict__ row, int E, int sub, bool vec, float (&x)[V]) {
   constexpr int VW = RowVec<T>::VW;
@@ -93,8 +93,6 @@ __device__ __forceinline__ void load_row(const T* __restrict__ row, int E, int s
       for (int i = 0; i < VW; ++i) x[b * VW + i] = c0 + i < E ? to_f32(row[c0 + i]) : -INFINITY;
     }
   }
-#pragma unroll
-  for (int v = 0; v < V; ++v) x[v] = fmaxf(x[v], -INFINITY);   // (the larger of a NaN and a number is the number)
 }
 template <typename T, int G, int V>
 __device__ __forceinline__ void store_row(T* __restrict__ row, int E, int sub, bool vec, const float (&x)[V]) {
@@ -157,32 +155,30 @@ __device__ __forceinline__ float rcp_hw(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// sigmoid(x), and 1 - sigmoid(x) in `rest` without cancellation.  The exponential is held in 2^126: beyond, sigmoid(x) is 2^-126.
-__device__ __forceinline__ float sigmoid_row(float x, float* rest = nullptr) {
-  const float e = exp2_hw(fminf(times_log2e(-x), 126.f)), s = rcp_hw(1.f + e);
-  if (rest) *rest = e * s;
-  return s;
-}
+__device__ __forceinline__ float sigmoid_row(float x) { return rcp_hw(1.f + exp_row(-x)); }
 
-// Unnormalised scores of a row on G lanes, in place, and their sum; `top` is the row's largest logit.
-//   softmax  e^(x - top).  Logits of +inf share the row, the limit of equal ones that grow: they score 1, all others 0.
-//   sigmoid  sigmoid(x); where all logits are below 0, sigmoid(x) e^-top: low ones underflow together, their shares do not.
-// (the caller's lanes of a group agree on `top`; rows of one warp may differ)
 template <int V>
-__device__ __forceinline__ float top_of(const float (&x)[V]) {
+__device__ __forceinline__ float top_of(const float (&x)[V]) {             // (the larger of a NaN and a number is the number)
   float top = x[0];
 #pragma unroll
   for (int v = 1; v < V; ++v) top = fmaxf(top, x[v]);
   return top;
 }
-__device__ __forceinline__ float score(int act, float x, float top) {      // of one logit
+// The score of one logit in a row whose largest is `top`; see scores().
+__device__ __forceinline__ float score(int act, float x, float top) {
   if (x == -INFINITY) return 0.f;
   if (act == MIX_ACT_SOFTMAX) return x == top ? 1.f : exp_row(x - top);
   return top >= 0.f ? sigmoid_row(x) : exp_row(x - top) * rcp_hw(1.f + exp_row(x));
 }
-// rest: where given and the scores are sigmoids, 1 - sigmoid of each logit
+// Unnormalised scores of a lane's logits, in place, and their sum.  A NaN scores 0: one that is there makes the sum a NaN, which is
+// looked at once for all V.
+//   softmax  e^(x - top), `top` the row's largest logit.  Logits of +inf share the row, the limit of equal ones that grow: they
+//            score 1, all others 0.
+//   sigmoid  sigmoid(x).  Where all logits of a row are so low that their sigmoids underflow, their shares do not: `low` says
+//            that the row's largest, below 0, is to be taken off, sigmoid(x) e^-top.
+// slope: where given, score times (1 - sigmoid) of sigmoids, the score itself of a softmax
 template <int V>
-__device__ __forceinline__ float scores(int act, float top, float (&x)[V], float (*rest)[V] = nullptr) {
+__device__ __forceinline__ float scores(int act, float top, bool low, float (&x)[V], float (*slope)[V] = nullptr) {
   float total = 0.f;
   if (act == MIX_ACT_SOFTMAX) {
     if (top == INFINITY) {
@@ -195,26 +191,41 @@ __device__ __forceinline__ float scores(int act, float top, float (&x)[V], float
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       x[v] = exp_row(x[v] - top);
+      if (slope) (*slope)[v] = x[v];
       total += x[v];
     }
-  } else if (top >= 0.f) {
+  } else if (!low) {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const float s = sigmoid_row(x[v], rest ? &(*rest)[v] : nullptr);
-      x[v] = x[v] == -INFINITY ? 0.f : s;
-      total += x[v];
+      const float e = exp_row(-x[v]), s = rcp_hw(1.f + e);
+      if (slope) (*slope)[v] = s * (fminf(e, 3e38f) * s);      // (where e is infinite s is 0)
+      x[v] = s;
+      total += s;
     }
   } else {
+    const float off = top < 0.f && top > -INFINITY ? top : 0.f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const float r = rcp_hw(1.f + exp_row(x[v]));
-      if (rest) (*rest)[v] = r;
-      x[v] = x[v] == -INFINITY ? 0.f : exp_row(x[v] - top) * r;
+      const float r = rcp_hw(1.f + exp_row(x[v])), s = off == 0.f ? sigmoid_row(x[v]) : exp_row(x[v] - off) * r;
+      if (slope) (*slope)[v] = s * r;
+      x[v] = s;
+      total += s;
+    }
+  }
+  if (total != total) {
+    total = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      if (x[v] != x[v]) {
+        x[v] = 0.f;
+        if (slope) (*slope)[v] = 0.f;
+      }
       total += x[v];
     }
   }
   return total;
 }
+constexpr float kLowTotal = 1e-20f;        // below it a row's sigmoids are taken again with `low`
 #endif
 
 constexpr int kOpMaxExperts = 512;

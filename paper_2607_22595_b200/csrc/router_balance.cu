@@ -105,8 +105,12 @@ balance_kernel(const T* __restrict__ logits, long long ld, int vec, const int* _
       }
       const bool on = group_any<G>(named);
       rows += on && sub == 0;
-      const float total = group_sum<G>(scores<V>(act, group_max<G>(top_of<V>(x)), x));
-      const float inv = on && total > 0.f ? 1.f / total : 0.f;
+      float total = group_sum<G>(scores<V>(act, act == MIX_ACT_SOFTMAX ? group_max<G>(top_of<V>(x)) : 0.f, false, x));
+      if (act == MIX_ACT_SIGMOID && __any_sync(0xffffffffu, on && total < kLowTotal)) {
+        if (t < b) load_row<T, G, V>(logits + t * ld, E, sub, vec != 0, x);
+        total = group_sum<G>(scores<V>(act, group_max<G>(top_of<V>(x)), true, x));
+      }
+      const float inv = on && total > 0.f ? rcp_hw(total) : 0.f;
 #pragma unroll
       for (int v = 0; v < V; ++v) acc[v] = fmaf(x[v], inv, acc[v]);
     }
@@ -347,26 +351,24 @@ balance_grad_kernel(const T* __restrict__ logits, long long ld, int vec, const i
     fetch(at, next, next_named);
     for (int base = at; base < b; base += R) {
       const int t = base + lane / G;
-      float x[V], rest[V];
+      float x[V], slope[V];
       const bool on = group_any<G>(next_named);
 #pragma unroll
       for (int v = 0; v < V; ++v) x[v] = next[v];
       if (base + R < b) fetch(base + R, next, next_named);
-      const float total = group_sum<G>(scores<V>(act, group_max<G>(top_of<V>(x)), x, &rest));
-      const float inv = on && total > 0.f ? 1.f / total : 0.f;
+      float total = group_sum<G>(scores<V>(act, act == MIX_ACT_SOFTMAX ? group_max<G>(top_of<V>(x)) : 0.f, false, x, &slope));
+      if (act == MIX_ACT_SIGMOID && __any_sync(0xffffffffu, on && total < kLowTotal)) {
+        if (t >= a && t < b) load_row<T, G, V>(logits + t * ld, E, sub, vec != 0, x);
+        total = group_sum<G>(scores<V>(act, group_max<G>(top_of<V>(x)), true, x, &slope));
+      }
+      const float inv = on && total > 0.f ? rcp_hw(total) : 0.f;
       float dot = 0.f;
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        x[v] *= inv;
-        dot = fmaf(f[v], x[v], dot);
-      }
-      dot = group_sum<G>(dot);
+      for (int v = 0; v < V; ++v) dot = fmaf(f[v], x[v], dot);
+      dot = group_sum<G>(dot) * inv;
+      const float by = inv != 0.f ? coef * inv : 0.f;          // (a row that is off stays 0, whatever its d_loss)
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        float d = coef * (x[v] * (f[v] - dot));
-        if (act == MIX_ACT_SIGMOID) d *= rest[v];
-        x[v] = x[v] > 0.f ? d : 0.f;                           // (0 where the row is off, whatever its d_loss)
-      }
+      for (int v = 0; v < V; ++v) x[v] = by * slope[v] * (f[v] - dot);
       if (t < b) store_row<T, G, V>(d_logits + t * ld_d, E, sub, vec_d != 0, x);
     }
     at = b;

@@ -46,7 +46,9 @@ router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_ro
 #pragma unroll
     for (int v = 0; v < V; ++v) x[v] = -INFINITY;
   }
-  const float lane_top = top_of<V>(x), top = group_max<G>(lane_top);
+#pragma unroll
+  for (int v = 0; v < V; ++v) x[v] = fmaxf(x[v], -INFINITY);               // a NaN is never chosen
+  const float top = group_max<G>(top_of<V>(x));
   int my_idx[S];
   float my_x[S];
 #pragma unroll
@@ -130,20 +132,20 @@ router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_ro
   }
   const bool plain = act == MIX_ACT_SIGMOID && !renorm;                    // the weight is the sigmoid itself
   float total = 0.f;
-  if (act == MIX_ACT_SOFTMAX && !renorm) total = scores<V>(act, top, x);
+  if (act == MIX_ACT_SOFTMAX && !renorm) total = scores<V>(act, top, false, x);
 #pragma unroll
   for (int s = 0; s < S; ++s) {
     my_x[s] = my_idx[s] < 0 ? 0.f : (plain ? sigmoid_row(my_x[s]) : score(act, my_x[s], top));
     if (renorm) total += my_x[s];
   }
   if (!plain) total = group_sum<G>(total);
-  const float norm = plain ? 1.f : total;
+  const float by = plain ? 1.f : rcp_hw(total);
 #pragma unroll
   for (int s = 0; s < S; ++s) {
     const int j = s * G + sub;
     if (j < k && t < T_rows) {
       idx[t * k + j] = my_idx[s];
-      weights[t * k + j] = my_idx[s] >= 0 ? my_x[s] / norm : 0.f;
+      weights[t * k + j] = my_idx[s] >= 0 ? my_x[s] * by : 0.f;
     }
   }
 }
@@ -203,8 +205,8 @@ router_topk_grad_kernel(const T* __restrict__ logits, long long ld, int vec, int
   for (int v = 0; v < V; ++v) d[v] = 0.f;
   if (dense) {
     any = group_any<G>(any);
-    const float total = group_sum<G>(scores<V>(act, group_max<G>(top_of<V>(p)), p));
-    const float inv = any && total > 0.f ? 1.f / total : 0.f;
+    const float total = group_sum<G>(scores<V>(act, group_max<G>(top_of<V>(p)), false, p));
+    const float inv = any && total > 0.f ? rcp_hw(total) : 0.f;
     const float less = S == 1 ? inv * -s : inv;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
