@@ -24,11 +24,11 @@ constexpr int kSelThreads = 256;
 // Rows of up to 128 experts: k rounds of an arg-max over the G lanes, 32 / G rows of a warp side by side.
 // Wider rows (a warp each) are bound by comparisons and selections, which issue at half rate, so they compare keys that carry the
 // column: the logit's order-preserving bits, the lowest 8 or 9 replaced by ~column.  No two are equal, a round is one reduction
-// over the warp, and a lane keeps its two largest keys; one that has given its first offers its second.  k + 1 rounds.  The row
-// is done again by rounds over all logits where that may not be the answer: a lane gave both and has more above the last key
-// (8 of 256: a row in twenty), or two neighbours of fp32 agree in all bits of the key (16-bit logits lose none).
-// 65536 rows of 256, k = 8, with the softmax over the row: 76 us by rounds over all logits, 37 with logits and columns apart, %s us
-// so; the logits' stream alone takes 10.3.
+// over the warp, and a lane keeps its three largest keys; one that has given its first offers its second.  k + 1 rounds.  The row
+// is done again by rounds over all logits where that may not be the answer: a lane gave all three and has more above the last key
+// (8 of 256: four rows in a thousand), or two neighbours of fp32 agree in all bits of the key (16-bit logits lose none).
+// 65536 rows of 256, k = 8, with the softmax over the row: 76 us by rounds over all logits, 37 with logits and columns apart, 35
+// with two keys a lane, %s us so; the logits' stream alone takes 10.3.
 template <typename T, int G, int V>
 __global__ void __launch_bounds__(kSelThreads)
 router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_rows, int E, int k, int act, int renorm,
@@ -46,9 +46,15 @@ router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_ro
 #pragma unroll
     for (int v = 0; v < V; ++v) x[v] = -INFINITY;
   }
+  float sum = 0.f;                                                         // a NaN is never chosen; one that is there makes the sum one
 #pragma unroll
-  for (int v = 0; v < V; ++v) x[v] = fmaxf(x[v], -INFINITY);               // a NaN is never chosen
-  const float top = group_max<G>(top_of<V>(x));
+  for (int v = 0; v < V; ++v) sum += x[v];
+  if (__any_sync(0xffffffffu, sum != sum)) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) x[v] = fmaxf(x[v], -INFINITY);             // (the larger of a NaN and a number is the number)
+  }
+  float top = 0.f;
+  if (G < 32) top = group_max<G>(top_of<V>(x));
   int my_idx[S];
   float my_x[S];
 #pragma unroll
@@ -58,7 +64,7 @@ router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_ro
     constexpr unsigned kCol = V * 32 - 1;                                  // the key's bits that hold ~column
     constexpr unsigned kNone = 0x007fffffu & ~kCol;                        // -inf's key
     static_assert((kCol & V * 32) == 0, "a power of two");
-    unsigned key[V], hi[V / 2], lo[V / 2];
+    unsigned key[V], k1[V / 2], k2[V / 2], k3[V / 4];                      // sorted parts of the lane's keys, their three largest
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const unsigned bits = __float_as_uint(x[v] + 0.f);                   // -0 and 0 are equal
@@ -66,18 +72,20 @@ router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_ro
     }
 #pragma unroll
     for (int i = 0; i < V / 2; ++i) {
-      hi[i] = max(key[2 * i], key[2 * i + 1]);
-      lo[i] = min(key[2 * i], key[2 * i + 1]);
+      k1[i] = max(key[2 * i], key[2 * i + 1]);
+      k2[i] = min(key[2 * i], key[2 * i + 1]);
     }
 #pragma unroll
     for (int n = V / 4; n > 0; n /= 2) {
 #pragma unroll
       for (int i = 0; i < n; ++i) {
-        lo[i] = max(min(hi[i], hi[i + n]), max(lo[i], lo[i + n]));
-        hi[i] = max(hi[i], hi[i + n]);
+        const unsigned m = min(k1[i], k1[i + n]), l = max(k2[i], k2[i + n]);
+        k1[i] = max(k1[i], k1[i + n]);
+        k2[i] = max(m, l);
+        k3[i] = n == V / 4 ? min(m, l) : max(min(m, l), max(k3[i], k3[i + n]));
       }
     }
-    unsigned first = hi[0], second = lo[0], last = 0u, mine = 0u;
+    unsigned first = k1[0], second = k2[0], third = k3[0], last = 0u, mine = 0u;
     int given = 0;
 #pragma unroll
     for (int j = 0; j < kOpMaxTopk + 1; ++j) {
@@ -87,16 +95,20 @@ router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_ro
       mine = j == sub ? last : mine;
       if (first == last) {
         first = second;
-        second = 0u;
+        second = third;
+        third = 0u;
         ++given;
       }
     }
-    last = max(last, kNone + kCol + 1u);
-    int above = 0;
+    bool unsure = false;
+    if (__any_sync(0xffffffffu, given > 2)) {
+      last = max(last, kNone + kCol + 1u);
+      int above = 0;
 #pragma unroll
-    for (int v = 0; v < V; ++v) above += key[v] >= last;
+      for (int v = 0; v < V; ++v) above += key[v] >= last;
+      unsure = above != given;
+    }
     const unsigned after = __shfl_down_sync(0xffffffffu, mine, 1);         // (by all lanes)
-    bool unsure = above != given;
     if (sizeof(T) == 4) unsure |= sub < k && mine != 0u && ((after ^ mine) & ~kCol) == 0u;
     rounds = __any_sync(0xffffffffu, unsure);
     if (!rounds && sub < k && mine != 0u) {
@@ -130,6 +142,7 @@ router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_ro
       }
     }
   }
+  if (G == 32) top = __shfl_sync(0xffffffffu, my_x[0], 0);                 // the first one chosen
   const bool plain = act == MIX_ACT_SIGMOID && !renorm;                    // the weight is the sigmoid itself
   float total = 0.f;
   if (act == MIX_ACT_SOFTMAX && !renorm) total = scores<V>(act, top, false, x);
