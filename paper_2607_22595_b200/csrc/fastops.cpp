@@ -137,19 +137,45 @@ struct Call {
     t = Tensor(at::detail::empty_cuda(shape, type, c10::Device(c10::kCUDA, (c10::DeviceIndex)device), std::nullopt));
     return t;
   }
-  // Given (checked) or new; `out` gets the new reference that is returned to the caller.
+  // The dense outputs of the call, in the order of the returned tuple: given (checked), or new.  New ones are pieces of one
+  // allocation, each on 256 bytes: an allocation and its tensor cost 0.8 us, a tensor on a piece 0.3.
+  struct Piece {
+    int64_t at;
+    ScalarType type;
+    at::DimVector shape;
+    void** p;
+    PyObject** out;
+  };
+  Piece piece[4];
+  int n_pieces = 0;
+  int64_t bytes = 0;
   template <typename T>
-  T* result(PyObject* given, const char* name, ScalarType type, std::initializer_list<int64_t> shape, const Tensor& like, PyObject** out) {
+  void want(PyObject* given, const char* name, ScalarType type, std::initializer_list<int64_t> shape, const Tensor& like, T** p, PyObject** out) {
     if (given != Py_None) {
-      T* p = dense<T>(given, name, type, shape, like);
+      *p = dense<T>(given, name, type, shape, like);
       Py_INCREF(given);
       *out = given;
-      return p;
+      return;
     }
-    Tensor& t = empty(shape, type);
-    *out = THPVariable_Wrap(t);
-    if (!*out) throw Raised();
-    return static_cast<T*>(t.data_ptr());
+    Piece& w = piece[n_pieces++];
+    int64_t n = sizeof(T);
+    for (const int64_t d : shape) n *= d;
+    w = Piece{bytes, type, at::DimVector(shape), reinterpret_cast<void**>(p), out};
+    bytes += (n + 255) / 256 * 256;
+  }
+  void allocate() {
+    if (n_pieces == 0) return;
+    const Tensor& all = empty({bytes}, ScalarType::Byte);
+    for (int i = 0; i < n_pieces; ++i) {
+      Piece& w = piece[i];
+      const caffe2::TypeMeta meta = c10::scalarTypeToTypeMeta(w.type);
+      Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(all.storage()), all.key_set(), meta);
+      t.unsafeGetTensorImpl()->set_sizes_contiguous(w.shape);
+      t.unsafeGetTensorImpl()->set_storage_offset(w.at / (int64_t)meta.itemsize());
+      *w.p = static_cast<char*>(all.data_ptr()) + w.at;
+      *w.out = THPVariable_Wrap(std::move(t));
+      if (!*w.out) throw Raised();
+    }
   }
   Rows result_rows(PyObject* given, const char* name, ScalarType type, int64_t n, int64_t m, const Tensor& like, PyObject** out) {
     if (given != Py_None) {
@@ -214,8 +240,11 @@ PyObject* router_topk(PyObject* const* a) {
   const int* live = a[4] == Py_None ? nullptr : dense<int>(a[4], "n_live", ScalarType::Int, {1}, x.t);
   Call c(x.t.get_device(), a[7]);
   Results r;
-  int* idx = c.result<int>(a[5], "idx", ScalarType::Int, {x.n, k}, x.t, &r.o[0]);
-  float* w = c.result<float>(a[6], "weights", ScalarType::Float, {x.n, k}, x.t, &r.o[1]);
+  int* idx;
+  float* w;
+  c.want(a[5], "idx", ScalarType::Int, {x.n, k}, x.t, &idx, &r.o[0]);
+  c.want(a[6], "weights", ScalarType::Float, {x.n, k}, x.t, &w, &r.o[1]);
+  c.allocate();
   c.run([&](void* s, char* e, int n) { return mix_router_topk(x.p, x.dtype, x.ld, (int)x.n, (int)x.m, (int)k, act, renorm, live, idx, w, s, e, n); });
   return r.tuple(2);
 }
@@ -250,9 +279,11 @@ PyObject* expert_order(PyObject* const* a) {
   if (bytes < 0) throw Failed{(int)bytes, "n_experts or the number of entries is out of range"};
   Call c(it.get_device(), a[5]);
   Results r;
-  int* offsets = c.result<int>(a[2], "offsets", ScalarType::Int, {E + 1}, it, &r.o[0]);
-  int* order = c.result<int>(a[3], "order", ScalarType::Int, {n}, it, &r.o[1]);
-  int* position = c.result<int>(a[4], "position", ScalarType::Int, {it.size(0), it.size(1)}, it, &r.o[2]);
+  int *offsets, *order, *position;
+  c.want(a[2], "offsets", ScalarType::Int, {E + 1}, it, &offsets, &r.o[0]);
+  c.want(a[3], "order", ScalarType::Int, {n}, it, &order, &r.o[1]);
+  c.want(a[4], "position", ScalarType::Int, {it.size(0), it.size(1)}, it, &position, &r.o[2]);
+  c.allocate();
   void* ws = c.scratch(bytes);
   c.run([&](void* s, char* e, int m) { return mix_expert_order(idx, n, (int)E, offsets, order, position, ws, bytes, s, e, m); });
   return r.tuple(3);
@@ -278,10 +309,13 @@ PyObject* router_balance(PyObject* const* a) {
   const int act = (int)integer(a[3], "act", 0, 2);
   Call c(x.t.get_device(), a[4]);
   Results r;
-  float* loss = c.result<float>(Py_None, "loss", ScalarType::Float, {n_seg}, x.t, &r.o[0]);
-  int* counts = c.result<int>(Py_None, "counts", ScalarType::Int, {n_seg, x.m}, x.t, &r.o[1]);
-  float* mean = c.result<float>(Py_None, "mean_p", ScalarType::Float, {n_seg, x.m}, x.t, &r.o[2]);
-  int* rows = c.result<int>(Py_None, "rows", ScalarType::Int, {n_seg}, x.t, &r.o[3]);
+  float *loss, *mean;
+  int *counts, *rows;
+  c.want(Py_None, "loss", ScalarType::Float, {n_seg}, x.t, &loss, &r.o[0]);
+  c.want(Py_None, "counts", ScalarType::Int, {n_seg, x.m}, x.t, &counts, &r.o[1]);
+  c.want(Py_None, "mean_p", ScalarType::Float, {n_seg, x.m}, x.t, &mean, &r.o[2]);
+  c.want(Py_None, "rows", ScalarType::Int, {n_seg}, x.t, &rows, &r.o[3]);
+  c.allocate();
   const long long bytes = mix_router_balance_workspace((int)x.n, (int)x.m, n_seg);
   void* ws = c.scratch(bytes);
   c.run([&](void* s, char* e, int n) {
@@ -325,8 +359,11 @@ PyObject* quantize_rows(PyObject* const* a) {
   const int k = (int)integer(a[2], "k", 1, INT_MAX);
   Call c(x.t.get_device(), a[5]);
   Results r;
-  int8_t* codes = c.result<int8_t>(a[3], "codes", ScalarType::Char, {n, x.m}, x.t, &r.o[0]);
-  float* scale = c.result<float>(a[4], "scale", ScalarType::Float, {n}, x.t, &r.o[1]);
+  int8_t* codes;
+  float* scale;
+  c.want(a[3], "codes", ScalarType::Char, {n, x.m}, x.t, &codes, &r.o[0]);
+  c.want(a[4], "scale", ScalarType::Float, {n}, x.t, &scale, &r.o[1]);
+  c.allocate();
   if (order && n == 0) return r.tuple(2);
   c.run([&](void* s, char* e, int len) {
     return mix_quantize_rows(x.p, x.dtype, x.ld, (int)x.n, order, k, (int)n, (int)x.m, reinterpret_cast<signed char*>(codes), scale, s, e, len);
