@@ -167,8 +167,15 @@ __device__ const long long g_i8_wait_cycles = kI8WaitCycles;
 // tokens' rows, so that a k-block of 256 tokens costs a CTA 32 KB of copies and 32 KB of reads of shared memory, not 48 and 48:
 // at 128 bytes a clock the single CTA's 96 KB take 768 clocks, while the tensor core needs 512 (measured 834 and 1573 us for
 // 8192 x 8192 x 32768).
-template <int NT, bool kPair>
+//
+// kSplit: the 2, 4 or 8 CTAs of a cluster work on one tile, each on its part of the codes of a row, for calls whose tiles leave most
+// SMs without one (4096 channels are 32).  The parts meet in shared memory, in 32-bit integers: where they are added up does not
+// show in the result.
+enum { kSingle = 0, kPairs = 1, kSplit = 2 };
+constexpr int kMostParts = 8;
+template <int NT, int kMode>
 struct GemmCfg {
+  static constexpr bool kPair = kMode == kPairs;
   static constexpr int kCtas = kPair ? 2 : 1;
   static constexpr int kTokRows = NT / kCtas;                  // rows of the token operand in this CTA's shared memory
   static constexpr int kBoxRows = kTokRows < 64 ? kTokRows : 64;   // tokens of a copy
@@ -177,6 +184,7 @@ struct GemmCfg {
   static constexpr int kStages = (200 * 1024) / kStageBytes < 12 ? (200 * 1024) / kStageBytes : 12;
   static constexpr int kTmemCols = 2 * NT < 32 ? 32 : 2 * NT;
   static constexpr int kSmem = kStages * kStageBytes + kEpiWarps * kStageOut + 1024;
+  static_assert(NT * kTileCh * 4 <= kStages * kStageBytes, "a part's sums fit where its operands were");
 };
 
 struct GemmShared {
@@ -219,16 +227,21 @@ struct I8Tile {
 // Tiles of an expert: groups of kGroup token tiles; in a group the channels one after the other, each with all of the group's
 // token tiles next to each other: a tile of W comes from DRAM once a group, and the group's tokens stay in L2.
 constexpr int kGroup = 16;
-template <int NT, bool kPair>
-__device__ __forceinline__ I8Tile i8_tile(const GemmShared* sh, int tile, int ch_tiles, int& e) {
-  while (tile >= sh->tile0[e + 1]) ++e;                        // (a role's tiles only rise)
-  const int local = tile - sh->tile0[e], rows = sh->row0[e + 1] - sh->row0[e], tt = (rows + NT - 1) / NT;
+__device__ __forceinline__ void i8_place(int local, int tt, int ch_tiles, int* ch, int* tk) {
   const int group = local / (kGroup * ch_tiles), in = local - group * kGroup * ch_tiles, wide = min(kGroup, tt - group * kGroup);
+  *ch = in / wide;
+  *tk = group * kGroup + in % wide;
+}
+template <bool kPair>
+__device__ __forceinline__ I8Tile i8_tile(const GemmShared* sh, int tile, int ch_tiles, int tile_tok, int& e) {
+  while (tile >= sh->tile0[e + 1]) ++e;                        // (a role's tiles only rise)
+  const int rows = sh->row0[e + 1] - sh->row0[e], tt = (rows + tile_tok - 1) / tile_tok;
+  int ch, tk;
+  i8_place(tile - sh->tile0[e], tt, ch_tiles, &ch, &tk);
   I8Tile t;
   t.expert = e;
   t.once = tt == 1;
-  t.ch0 = in / wide * (kPair ? 2 * kTileCh : kTileCh);
-  const int tk = group * kGroup + in % wide;
+  t.ch0 = ch * (kPair ? 2 * kTileCh : kTileCh);
   // an expert's rows are dealt evenly: with a full tile and a small one in turn, the even workers would get all the full ones
   const int each = ((rows + tt - 1) / tt + 15) & ~15;
   t.row0 = sh->row0[e] + tk * each;
@@ -236,12 +249,13 @@ __device__ __forceinline__ I8Tile i8_tile(const GemmShared* sh, int tile, int ch
   return t;
 }
 
-template <typename OutT, int NT, bool kPair>
+template <typename OutT, int NT, int kMode>
 __global__ void __launch_bounds__(kGemmThreads, 1)
 linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x, const float* __restrict__ scale,
                   const float* __restrict__ w_scale, const float* __restrict__ bias, const int* __restrict__ offsets, int n_rows, int K,
-                  int N, int E, OutT* __restrict__ out, long long ld_out, int vec) {
-  using Cfg = GemmCfg<NT, kPair>;
+                  int N, int E, int tile_tok, int parts, OutT* __restrict__ out, long long ld_out, int vec) {
+  using Cfg = GemmCfg<NT, kMode>;
+  constexpr bool kPair = Cfg::kPair;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* ring = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   __shared__ GemmShared shared;
@@ -249,7 +263,9 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
   GemmShared* sh = &shared;
   const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int rank = kPair ? (int)cluster_ctarank() : 0;         // rank 0 leads a pair: it issues the instructions, and its barriers count both CTAs' copies
-  const int worker = kPair ? (int)(blockIdx.x >> 1) : (int)blockIdx.x, n_workers = kPair ? (int)(gridDim.x >> 1) : (int)gridDim.x;
+  const int part = kMode == kSplit ? (int)cluster_ctarank() : 0;
+  const int share = kPair ? 2 : (kMode == kSplit ? parts : 1);
+  const int worker = (int)blockIdx.x / share, n_workers = (int)gridDim.x / share;
   if (threadIdx.x == 0) {
     for (int s = 0; s < Cfg::kStages; ++s) {
       mbar_init(smem_u32(&sh->full[s]), 1);
@@ -267,10 +283,21 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
     if (kPair) tmem_alloc_pair(smem_u32(&sh->tmem_base), Cfg::kTmemCols);
     else tmem_alloc(smem_u32(&sh->tmem_base), Cfg::kTmemCols);
   }
-  pdl_wait();
-  pdl_launch_dependents();
   constexpr int kChannels = kTileCh * Cfg::kCtas;
   const int ch_tiles = (N + kChannels - 1) / kChannels;
+  const int num_kb = (K + kKBytes - 1) / kKBytes;
+  const int kb0 = kMode == kSplit ? num_kb * part / parts : 0, kb1 = kMode == kSplit ? num_kb * (part + 1) / parts : num_kb;
+  if (NT <= 64 && warp == 0 && offsets == nullptr) {
+    // A few tokens: the stream of W is what takes the time.  While the kernel in front of this one still runs, its first lines are
+    // fetched into L2 -- no further: W may be what that kernel writes, and L2 is where its writes arrive.
+    int ch, tk;
+    i8_place(worker, (n_rows + tile_tok - 1) / tile_tok, ch_tiles, &ch, &tk);
+    if (kb0 + lane < kb1)
+      asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];"
+                   ::"l"(&tmap_w), "r"((kb0 + lane) * kKBytes), "r"(ch * kChannels + rank * kTileCh) : "memory");
+  }
+  pdl_wait();
+  pdl_launch_dependents();
   if (warp == 0) {                                             // the experts' rows and tiles; offsets that fall or leave the rows are held in
     int row = 0, tiles = 0;
     for (int e0 = 0; e0 < E; e0 += 32) {
@@ -286,7 +313,7 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
       end = max(end, row);
       int prev = __shfl_up_sync(0xffffffffu, end, 1);
       if (lane == 0) prev = row;
-      int n = e < E ? (end - prev + NT - 1) / NT * ch_tiles : 0;
+      int n = e < E ? (end - prev + tile_tok - 1) / tile_tok * ch_tiles : 0;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const int y = __shfl_up_sync(0xffffffffu, n, o);
@@ -310,7 +337,6 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
   tc_fence_after();
   const unsigned tmem_base = (unsigned)uniform((int)sh->tmem_base);
   const int total = uniform(sh->tile0[E]);
-  const int num_kb = (K + kKBytes - 1) / kKBytes;
   const long long* cap = &g_i8_wait_cycles;
 
   if (warp == 0) {
@@ -319,7 +345,7 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
     bool ok = true;
     const unsigned long long stream = l2_evict_first();
     for (int tile = worker; tile < total && ok; tile += n_workers) {
-      const I8Tile t = i8_tile<NT, kPair>(sh, tile, ch_tiles, e);
+      const I8Tile t = i8_tile<kPair>(sh, tile, ch_tiles, tile_tok, e);
       if (t.n_tok <= 0) continue;
       const int tok_rows = kPair ? ((t.n_tok + 31) & ~31) / 2 : t.n_tok;     // of this CTA
       const int boxes = uniform((tok_rows + Cfg::kBoxRows - 1) / Cfg::kBoxRows);
@@ -328,7 +354,7 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
       const int wy = uniform(t.expert * N + t.ch0 + rank * kTileCh), xy = uniform(t.row0 + (kPair ? rank * tok_rows : 0));
       const bool once = uniform((int)t.once) != 0;             // (then what the kernels around this one share stays in L2)
       const unsigned bytes = (Cfg::kABytes + boxes * Cfg::kBoxRows * kKBytes) * Cfg::kCtas;
-      for (int kb = 0; kb < num_kb; ++kb) {
+      for (int kb = kb0; kb < kb1; ++kb) {
         if (!mbar_wait_bounded_warp(smem_u32(&sh->empty[stage]), phase ^ 1u, &sh->abort_flag, cap, &g_i8_status)) { ok = false; break; }
         const unsigned bar = smem_u32(&sh->full[stage]), sa = smem_u32(ring + stage * Cfg::kStageBytes), on = elect_one();
         if (kPair) {
@@ -354,13 +380,13 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
       unsigned phase = 0, acc = 0, acc_phase = 0;
       bool ok = true;
       for (int tile = worker; tile < total && ok; tile += n_workers) {
-        const I8Tile t = i8_tile<NT, kPair>(sh, tile, ch_tiles, e);
+        const I8Tile t = i8_tile<kPair>(sh, tile, ch_tiles, tile_tok, e);
         if (t.n_tok <= 0) continue;
         const unsigned idesc = (unsigned)uniform((int)(kPair ? idesc_i8(2 * kTileCh, (t.n_tok + 31) & ~31) : idesc_i8(kTileCh, (t.n_tok + 15) & ~15)));
         if (!mbar_wait_bounded_warp(smem_u32(&sh->acc_empty[acc]), acc_phase ^ 1u, &sh->abort_flag, cap, &g_i8_status)) break;
         tc_fence_after();
         const unsigned d_tmem = tmem_base + acc * NT;
-        for (int kb = 0; kb < num_kb; ++kb) {
+        for (int kb = kb0; kb < kb1; ++kb) {
           if (!mbar_wait_bounded_warp(smem_u32(&sh->full[stage]), phase, &sh->abort_flag, cap, &g_i8_status)) { ok = false; break; }
           tc_fence_after();
           const unsigned sa = smem_u32(ring + stage * Cfg::kStageBytes);
@@ -368,8 +394,8 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
           const unsigned on = elect_one();
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            if (kPair) umma_i8_pair(d_tmem, da + 2ull * k, db + 2ull * k, idesc, (unsigned)((kb | k) != 0), on);
-            else umma_i8(d_tmem, da + 2ull * k, db + 2ull * k, idesc, (unsigned)((kb | k) != 0), on);
+            if (kPair) umma_i8_pair(d_tmem, da + 2ull * k, db + 2ull * k, idesc, (unsigned)((kb - kb0) | k) != 0u, on);
+            else umma_i8(d_tmem, da + 2ull * k, db + 2ull * k, idesc, (unsigned)((kb - kb0) | k) != 0u, on);
           }
           if (kPair) umma_commit_pair(smem_u32(&sh->empty[stage]), on);      // the stage is free again, in both CTAs
           else umma_commit(smem_u32(&sh->empty[stage]), on);
@@ -395,7 +421,7 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
     float* my_scale = tok_scale[warp - 2];
     OutT* piece = reinterpret_cast<OutT*>(ring + Cfg::kStages * Cfg::kStageBytes + (warp - 2) * kStageOut);
     for (int tile = worker; tile < total; tile += n_workers) {
-      const I8Tile t = i8_tile<NT, kPair>(sh, tile, ch_tiles, e);
+      const I8Tile t = i8_tile<kPair>(sh, tile, ch_tiles, tile_tok, e);
       if (t.n_tok <= 0) continue;
       const int ch0 = t.ch0 + rank * kTileCh + q * 32, ch = ch0 + lane;
       const bool valid = ch < N;
@@ -407,6 +433,17 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
       if (!mbar_wait_bounded_warp(smem_u32(&sh->acc_full[acc]), acc_phase, &sh->abort_flag, cap, &g_i8_status)) break;
       tc_fence_after();
       const unsigned taddr = tmem_base + acc * NT + ((unsigned)(q * 32) << 16);
+      if (kMode == kSplit) {                                   // the part's sums, [token][channel], where the operands were (all of them are used up)
+        int* sums = reinterpret_cast<int*>(ring) + q * 32 + lane;
+        for (int c0 = half * 32; c0 < t.n_tok; c0 += 64) {
+          float v[32];
+          tmem_ld32(taddr + c0, v);
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (c0 + i < t.n_tok) sums[(c0 + i) * kTileCh] = __float_as_int(v[i]);
+        }
+        continue;                                              // (a call has a tile per cluster at most)
+      }
       for (int c0 = half * 32; c0 < t.n_tok; c0 += 64) {
         float v[32];
         tmem_ld32(taddr + c0, v);
@@ -453,6 +490,47 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
   if (sh->abort_flag) {                                        // copies in flight land before shared memory is released
     const long long t0 = clock64();
     while (clock64() - t0 < 2000000ll) __nanosleep(1000);
+  }
+  if (kMode == kSplit) {
+    cluster_sync_all();
+    if (worker < total) {                                      // (the same in all CTAs of the cluster) every part writes its share of the tokens
+      int e = 0;
+      const I8Tile t = i8_tile<kPair>(sh, worker, ch_tiles, tile_tok, e);
+      const unsigned sums = smem_u32(ring);
+      for (int i = threadIdx.x; i < (t.n_tok - part + parts - 1) / parts * (kTileCh / 4); i += kGemmThreads) {   // four channels of a token
+        const int row = part + i / (kTileCh / 4) * parts, c = i % (kTileCh / 4) * 4, ch = t.ch0 + c;
+        if (ch >= N) continue;
+        int4 sum[kMostParts];
+#pragma unroll
+        for (int r = 0; r < kMostParts; ++r) {
+          sum[r] = make_int4(0, 0, 0, 0);
+          if (r < parts)
+            asm volatile("ld.shared::cluster.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(sum[r].x), "=r"(sum[r].y), "=r"(sum[r].z), "=r"(sum[r].w)
+                         : "r"(mapa_cluster(sums + (row * kTileCh + c) * 4, r)));
+        }
+        int all[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int r = 0; r < kMostParts; ++r) {
+          all[0] += sum[r].x;
+          all[1] += sum[r].y;
+          all[2] += sum[r].z;
+          all[3] += sum[r].w;
+        }
+        const float by = scale[t.row0 + row];
+        const long long w = (long long)t.expert * N + ch;
+        __align__(16) OutT v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = ch + j < N ? from_f32<OutT>(fmaf((float)all[j] * by, w_scale[w + j], bias ? bias[w + j] : 0.f)) : from_f32<OutT>(0.f);
+        OutT* dst = out + (long long)(t.row0 + row) * ld_out + ch;
+        if (vec && ch + 4 <= N) {
+          if (sizeof(OutT) == 4) *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(v);
+          else *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(v);
+        } else {
+          for (int j = 0; j < 4 && ch + j < N; ++j) dst[j] = v[j];
+        }
+      }
+    }
+    cluster_sync_all();                                        // the sums stay until they have been read
   }
   if (kPair) cluster_sync_all();                               // neither CTA's barriers or tensor memory go while the other may still reach them
   if (warp == 1) {
@@ -526,32 +604,43 @@ struct Gemm {
   long long ld_out;
 };
 
-template <typename OutT, int NT, bool kPair>
-cudaError_t gemm_launch(const Gemm& g, int dev, int n_sms, cudaStream_t s) {
-  using Cfg = GemmCfg<NT, kPair>;
+long long div_up(long long a, long long b) { return (a + b - 1) / b; }
+// Tiles of a call, at most, however the rows fall on the experts.
+long long tiles_at_most(const Gemm& g, int tile_tok, int channels) {
+  const long long tok = g.E == 1 ? div_up(g.n_rows, tile_tok) : (long long)g.n_rows / tile_tok + (g.E < g.n_rows ? g.E : g.n_rows);
+  return tok * div_up(g.N, channels);
+}
+
+// Tokens of a tile, and the parts of its codes.
+struct TilePlan {
+  int mode, nt, tile_tok, parts;
+};
+
+template <typename OutT, int NT, int kMode>
+cudaError_t gemm_launch(const Gemm& g, const TilePlan& p, int dev, int n_sms, cudaStream_t s) {
+  using Cfg = GemmCfg<NT, kMode>;
   static std::atomic<int> ready[kOpDevices];
   if (!ready[dev].load(std::memory_order_relaxed)) {
-    const cudaError_t e = cudaFuncSetAttribute(linear_int_kernel<OutT, NT, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem);
+    const cudaError_t e = cudaFuncSetAttribute(linear_int_kernel<OutT, NT, kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem);
     if (e != cudaSuccess) return e;
     ready[dev].store(1, std::memory_order_relaxed);
   }
   CUtensorMap tw, tx;
   if (make_tmap_i8(&tw, g.w, (unsigned long long)g.E * g.N, g.K, kTileCh) != MIX_OK || make_tmap_i8(&tx, g.codes, g.n_rows, g.K, Cfg::kBoxRows) != MIX_OK)
     return cudaErrorInvalidValue;
-  const long long tok_tiles = (long long)g.n_rows / NT + (g.E < g.n_rows ? g.E : g.n_rows);      // at most, however the rows fall
-  const long long most = (g.E == 1 ? (g.n_rows + NT - 1) / NT : tok_tiles) * ((g.N + kTileCh * Cfg::kCtas - 1) / (kTileCh * Cfg::kCtas));
-  const long long workers = n_sms / Cfg::kCtas;
+  const int ctas = kMode == kSplit ? p.parts : Cfg::kCtas;
+  const long long most = tiles_at_most(g, p.tile_tok, kTileCh * Cfg::kCtas), workers = n_sms / ctas;
   const int vec = (((uintptr_t)g.out | (uintptr_t)(g.ld_out * (long long)sizeof(OutT))) & 15u) == 0;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((most < workers ? most : workers) * Cfg::kCtas));
+  cfg.gridDim = dim3((unsigned)((most < workers ? most : workers) * ctas));
   cfg.blockDim = dim3(kGemmThreads);
   cfg.dynamicSmemBytes = Cfg::kSmem;
   cfg.stream = s;
   cudaLaunchAttribute at[2];
   int n_at = 0;
-  if (kPair) {
+  if (ctas > 1) {
     at[n_at].id = cudaLaunchAttributeClusterDimension;
-    at[n_at].val.clusterDim.x = 2;
+    at[n_at].val.clusterDim.x = ctas;
     at[n_at].val.clusterDim.y = 1;
     at[n_at++].val.clusterDim.z = 1;
   }
@@ -561,17 +650,54 @@ cudaError_t gemm_launch(const Gemm& g, int dev, int n_sms, cudaStream_t s) {
   }
   cfg.attrs = at;
   cfg.numAttrs = n_at;
-  return cudaLaunchKernelEx(&cfg, linear_int_kernel<OutT, NT, kPair>, tw, tx, g.scale, g.w_scale, g.bias, g.offsets, g.n_rows, g.K, g.N, g.E,
-                            static_cast<OutT*>(g.out), g.ld_out, vec);
+  return cudaLaunchKernelEx(&cfg, linear_int_kernel<OutT, NT, kMode>, tw, tx, g.scale, g.w_scale, g.bias, g.offsets, g.n_rows, g.K, g.N, g.E,
+                            p.tile_tok, p.parts, static_cast<OutT*>(g.out), g.ld_out, vec);
+}
+
+// A k-block of a tile of n tokens costs a CTA max(2 n, 256 + n) clocks in a pair and 256 + 2 n alone: the instructions take 2 n, and
+// shared memory moves each operand byte twice at 128 bytes a clock.  What a tile costs beside its k-blocks is some 1500 clocks, and
+// 2500 + 60 n more where its parts have to meet.  Among the tile sizes the one is taken whose waves cost least.  (1000 x 5120 codes by
+// 9992 channels: five tiles of 200 tokens instead of four of 250, 4 waves' worth instead of 4.5: %s us, 42 before; 16 x 4096 by 4096
+// channels: in four parts %s us, %s in one.)
+// By experts the host knows the rows' average alone: tiles as large as an even share, in pairs above 128 tokens.
+TilePlan tile_plan(const Gemm& g, int n_sms) {
+  const long long kbs = div_up(g.K, kKBytes);
+  TilePlan best = {kSingle, 32, 32, 1};
+  double least = 1e30;
+  const auto consider = [&](int mode, int nt, int tile_tok, int parts) {
+    const long long tiles = tiles_at_most(g, tile_tok, mode == kPairs ? 2 * kTileCh : kTileCh);
+    if (parts > 1 && (tiles * parts > n_sms || kbs < 4 * parts)) return;
+    const long long waves = parts > 1 ? 1 : div_up(tiles, mode == kPairs ? n_sms / 2 : n_sms);
+    const long long n = div_up(g.n_rows, div_up(g.n_rows, tile_tok)), a = mode == kPairs ? (2 * n > 256 + n ? 2 * n : 256 + n) : 256 + 2 * n;
+    const double cost = (double)waves * (double)(div_up(kbs, parts) * a + (parts > 1 ? 4000 + 60 * n : 1500));
+    if (cost < least) {
+      least = cost;
+      best = TilePlan{mode, nt, tile_tok, parts};
+    }
+  };
+  if (g.E == 1) {
+    for (int nt = 32; nt <= 128; nt *= 2)
+      for (int parts = 1; parts <= kMostParts; parts *= 2) consider(parts > 1 ? kSplit : kSingle, nt, nt, parts);
+    const long long fewest = div_up(g.n_rows, 256);
+    for (long long tt = fewest; tt < fewest + 8; ++tt) consider(kPairs, 256, (int)(div_up(div_up(g.n_rows, tt), 32) * 32), 1);
+    return best;
+  }
+  const int even = (int)div_up(g.n_rows, g.E);
+  if (even > 128) return TilePlan{kPairs, 256, 256, 1};
+  const int nt = even <= 32 ? 32 : (even <= 64 ? 64 : 128);
+  for (int parts = 1; parts <= kMostParts; parts *= 2) consider(parts > 1 ? kSplit : kSingle, nt, nt, parts);
+  return best;
 }
 
 template <typename OutT>
 cudaError_t gemm_pick(const Gemm& g, int dev, int n_sms, cudaStream_t s) {
-  const int share = (g.n_rows + g.E - 1) / g.E;
-  if (share <= 32) return gemm_launch<OutT, 32, false>(g, dev, n_sms, s);
-  if (share <= 64) return gemm_launch<OutT, 64, false>(g, dev, n_sms, s);
-  if (share <= 128) return gemm_launch<OutT, 128, false>(g, dev, n_sms, s);
-  return gemm_launch<OutT, 256, true>(g, dev, n_sms, s);
+  const TilePlan p = tile_plan(g, n_sms);
+  if (p.mode == kPairs) return gemm_launch<OutT, 256, kPairs>(g, p, dev, n_sms, s);
+  if (p.mode == kSplit)
+    return p.nt == 32 ? gemm_launch<OutT, 32, kSplit>(g, p, dev, n_sms, s)
+                      : (p.nt == 64 ? gemm_launch<OutT, 64, kSplit>(g, p, dev, n_sms, s) : gemm_launch<OutT, 128, kSplit>(g, p, dev, n_sms, s));
+  return p.nt == 32 ? gemm_launch<OutT, 32, kSingle>(g, p, dev, n_sms, s)
+                    : (p.nt == 64 ? gemm_launch<OutT, 64, kSingle>(g, p, dev, n_sms, s) : gemm_launch<OutT, 128, kSingle>(g, p, dev, n_sms, s));
 }
 
 int gemm_call(const Gemm& g, int dtype, void* stream, char* errbuf, int errbuf_len) {

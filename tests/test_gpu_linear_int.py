@@ -38,7 +38,8 @@ def _product(codes, scale, W, w_scale, bias=None):
 
 @pytest.mark.parametrize("T,K,N", [(1, 16, 1), (1, 4096, 1000), (2, 32, 7), (15, 128, 128), (16, 144, 130), (17, 112, 300), (31, 1008, 129), (33, 256, 64),
                                    (64, 4096, 512), (65, 528, 1111), (127, 128, 2), (128, 640, 257), (129, 2048, 384), (200, 16, 640), (255, 272, 1000),
-                                   (257, 1024, 255), (600, 1296, 777), (1030, 512, 2050), (3, 8192, 128), (300, 131056, 3)])
+                                   (257, 1024, 255), (600, 1296, 777), (1030, 512, 2050), (3, 8192, 128), (300, 131056, 3), (16, 8192, 4096), (50, 2064, 1000),
+                                   (100, 4096, 1500), (130, 4096, 3000), (333, 1024, 5000), (1000, 2048, 9000), (4200, 144, 300)])
 @pytest.mark.parametrize("dtype,bias", [("bf16", False), ("fp16", True), ("fp32", True)])
 def test_product(T, K, N, dtype, bias):
     codes, scale, W, w_scale = _operands(T, K, N, T + K + N)
@@ -201,7 +202,7 @@ def _counts(kind, E, seed):
 
 @pytest.mark.parametrize("E,kind", [(1, "even"), (2, "one"), (3, "large"), (8, "even"), (8, "few"), (8, "ragged"), (5, "large"), (33, "ragged"), (64, "few"),
                                     (100, "one"), (512, "few")])
-@pytest.mark.parametrize("K,N,dtype,bias", [(64, 48, "bf16", False), (208, 129, "fp16", True), (512, 384, "fp32", False)])
+@pytest.mark.parametrize("K,N,dtype,bias", [(64, 48, "bf16", False), (208, 129, "fp16", True), (512, 384, "fp32", False), (4112, 160, "bf16", True)])
 def test_grouped_product(E, kind, K, N, dtype, bias):
     counts = _counts(kind, E, E)
     front, tail = (3, 7) if E % 2 else (0, 0)
