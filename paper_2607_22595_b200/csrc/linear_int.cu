@@ -287,15 +287,6 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
   const int ch_tiles = (N + kChannels - 1) / kChannels;
   const int num_kb = (K + kKBytes - 1) / kKBytes;
   const int kb0 = kMode == kSplit ? num_kb * part / parts : 0, kb1 = kMode == kSplit ? num_kb * (part + 1) / parts : num_kb;
-  if (NT <= 64 && warp == 0 && offsets == nullptr) {
-    // A few tokens: the stream of W is what takes the time.  While the kernel in front of this one still runs, its first lines are
-    // fetched into L2 -- no further: W may be what that kernel writes, and L2 is where its writes arrive.
-    int ch, tk;
-    i8_place(worker, (n_rows + tile_tok - 1) / tile_tok, ch_tiles, &ch, &tk);
-    if (kb0 + lane < kb1)
-      asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];"
-                   ::"l"(&tmap_w), "r"((kb0 + lane) * kKBytes), "r"(ch * kChannels + rank * kTileCh) : "memory");
-  }
   pdl_wait();
   pdl_launch_dependents();
   if (warp == 0) {                                             // the experts' rows and tiles; offsets that fall or leave the rows are held in

@@ -266,9 +266,9 @@ router_topk_grad_kernel(const T* __restrict__ logits, long long ld, int vec, int
 }
 
 // ---------------------------------------------------------------------------------------------------- order by expert
-constexpr int kOrdThreads = 1024;
+constexpr int kOrdThreads = 512;
 constexpr int kOrdWarps = kOrdThreads / 32;
-constexpr int kOrdSteps = 8;                                    // entries a lane takes
+constexpr int kOrdSteps = 4;                                    // entries a lane takes
 constexpr int kOrdChunk = kOrdThreads * kOrdSteps;              // entries a CTA takes, at most
 constexpr int kOrdBuckets = kOpMaxExperts + 1;                  // the last of a call's holds the entries without an expert
 constexpr int kOrdCluster = 8;                                  // CTAs that can look into each other's counts
@@ -298,9 +298,53 @@ expert_hist_kernel(const int* __restrict__ idx, int n, int E, int steps, int* __
   for (int i = threadIdx.x; i < hist_stride(E); i += threads) hist[(size_t)blockIdx.x * hist_stride(E) + i] = i <= E ? h[i] : 0;
 }
 
+// For many chunks: the counts of a chunk become those of the chunks in front of it, in place; the row behind the last chunk receives
+// the sums over all.  A CTA has 32 buckets, a thread every bucket's chunks of one of 32 stretches.
+constexpr int kScanThreads = 1024;
+__global__ void __launch_bounds__(kScanThreads)
+expert_scan_kernel(int* __restrict__ hist, int n_chunks, int stride) {
+  __shared__ int part[kScanThreads / 32][33];
+  pdl_wait();
+  pdl_launch_dependents();
+  const int b = blockIdx.x * 32 + (threadIdx.x & 31), r = threadIdx.x >> 5;
+  const int each = (n_chunks + kScanThreads / 32 - 1) / (kScanThreads / 32), c0 = min(n_chunks, r * each), c1 = min(n_chunks, c0 + each);
+  int sum = 0;
+  if (b < stride) {
+#pragma unroll 8
+    for (int c = c0; c < c1; ++c) sum += hist[(size_t)c * stride + b];
+  }
+  part[r][threadIdx.x & 31] = sum;
+  __syncthreads();
+  if (r == 0) {
+    int run = 0;
+#pragma unroll
+    for (int i = 0; i < kScanThreads / 32; ++i) {
+      const int v = part[i][threadIdx.x];
+      part[i][threadIdx.x] = run;
+      run += v;
+    }
+    if (b < stride) hist[(size_t)n_chunks * stride + b] = run;
+  }
+  __syncthreads();
+  if (b < stride) {
+    int run = part[r][threadIdx.x & 31];
+    for (int c = c0; c < c1; c += 8) {
+      int v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = c + i < c1 ? hist[(size_t)(c + i) * stride + b] : 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (c + i < c1) hist[(size_t)(c + i) * stride + b] = run;
+        run += v[i];
+      }
+    }
+  }
+}
+
 // Entry i of the CTA's chunk goes to  (entries of lower experts) + (entries of this expert in earlier chunks, in earlier warps
 // of the CTA, earlier in the warp).  The counts of the other chunks: up to eight chunks are one cluster, whose CTAs read them from
-// each other's shared memory -- a call of up to 16384 entries is this one launch -- and beyond that expert_hist_kernel's.
+// each other's shared memory -- a call of up to 16384 entries is this one launch -- beyond that they are expert_hist_kernel's, and
+// of more than 64 chunks summed up by expert_scan_kernel.
 // A chunk is sorted in shared memory and leaves expert by expert: written straight from the registers every entry of a warp goes to
 // another line, which took an SM 8192 turns, half of the kernel's time.
 // A warp takes `steps` times 32 entries, the last warps of a call's last chunk fewer.
@@ -312,7 +356,7 @@ struct OrderShared {
 };
 template <bool kCluster>
 __global__ void __launch_bounds__(kOrdThreads)
-expert_order_kernel(const int* __restrict__ idx, int n, int E, const int* __restrict__ hist, int n_chunks, int steps, int* __restrict__ offsets,
+expert_order_kernel(const int* __restrict__ idx, int n, int E, const int* __restrict__ hist, int n_chunks, int steps, int scanned, int* __restrict__ offsets,
                     int* __restrict__ order, int* __restrict__ position) {
   extern __shared__ __align__(16) unsigned char order_smem[];
   OrderShared* sh = reinterpret_cast<OrderShared*>(order_smem);
@@ -380,6 +424,11 @@ expert_order_kernel(const int* __restrict__ idx, int n, int E, const int* __rest
       }
       sh->total[e] = all;
       sh->before[e] = pre;
+    }
+  } else if (scanned) {
+    for (int e = threadIdx.x; e <= E; e += blockDim.x) {
+      sh->before[e] = hist[(size_t)blockIdx.x * hist_stride(E) + e];
+      sh->total[e] = hist[(size_t)n_chunks * hist_stride(E) + e];
     }
   } else if (n_chunks > 1) {                             // four columns a thread, the chunks dealt to the threads left over
     const int wide = hist_stride(E) / 4, parts = (int)blockDim.x / wide, part = threadIdx.x / wide, col = threadIdx.x % wide;
@@ -517,14 +566,14 @@ extern "C" int mix_router_topk_grad(const void* logits, int dtype, long long ld,
 
 namespace {
 // How a call's entries are dealt.  What a step of a warp costs is instructions, some 90, so a chunk is small and many SMs share the
-// work: 16384 entries on 8 SMs of 512 threads, beyond that chunks of 2048 or 4096 entries as long as there are no more than 64 of
-// them -- every CTA reads all chunks' counts.  (65536 entries of 256 experts: %s us, 12.5 in eight chunks of 8192; 16384: %s, 12.3 in two.)
+// work: 16384 entries are on 8 SMs of 512 threads, beyond that chunks of 2048.  (65536 entries of 256 experts: %s us, 12.5 in eight
+// chunks of 8192; 16384: %s, 12.3 in two; 524288: %s, 14.9 in 64 chunks of 8192 whose CTAs add up all chunks' counts.)
 struct OrderPlan {
   int threads, steps, chunks;
-  bool cluster, counts;
+  bool cluster, counts, scan;
 };
 OrderPlan order_plan(long long n) {
-  OrderPlan p = {kOrdThreads, kOrdSteps, 1, false, false};
+  OrderPlan p = {512, 4, 1, false, false, false};
   const auto chunks = [&](int threads, int steps) { return (int)((n + threads * steps - 1) / (threads * steps)); };
   if (n <= 512) {
     p.threads = n <= 64 ? 64 : (int)((n + 31) / 32 * 32);
@@ -536,9 +585,8 @@ OrderPlan order_plan(long long n) {
     p.chunks = chunks(p.threads, p.steps);
     p.cluster = p.chunks > 1;
   } else {
-    if (chunks(512, 4) <= 64) { p.threads = 512; p.steps = 4; }
-    else if (chunks(512, 8) <= 64) { p.threads = 512; }
     p.chunks = chunks(p.threads, p.steps);
+    p.scan = p.chunks > 64;
     p.counts = true;
   }
   return p;
@@ -548,7 +596,7 @@ OrderPlan order_plan(long long n) {
 extern "C" long long mix_expert_order_workspace(long long n, int n_experts) {
   if (n < 0 || n > MIX_ORDER_MAX_ENTRIES || n_experts < 1 || n_experts > kOpMaxExperts) return MIX_ERR_OUT_OF_RANGE;
   const OrderPlan p = order_plan(n);
-  return p.counts ? (long long)p.chunks * hist_stride(n_experts) * (long long)sizeof(int) : 0;
+  return p.counts ? (long long)(p.chunks + 1) * hist_stride(n_experts) * (long long)sizeof(int) : 0;
 }
 
 extern "C" int mix_expert_order(const int* idx, long long n, int n_experts, int* offsets, int* order, int* position, void* workspace,
@@ -571,6 +619,7 @@ extern "C" int mix_expert_order(const int* idx, long long n, int n_experts, int*
     ready[dev].store(1, std::memory_order_relaxed);
   }
   if (p.counts) MIX_OP_CUDA(launch_pdl(kPdlHook, expert_hist_kernel, dim3(p.chunks), dim3(p.threads), 0, s, idx, (int)n, n_experts, p.steps, hist));
+  if (p.scan) MIX_OP_CUDA(launch_pdl(kPdlHook, expert_scan_kernel, dim3((hist_stride(n_experts) + 31) / 32), dim3(kScanThreads), 0, s, hist, p.chunks, hist_stride(n_experts)));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(p.chunks);
   cfg.blockDim = dim3(p.threads);
@@ -591,6 +640,6 @@ extern "C" int mix_expert_order(const int* idx, long long n, int n_experts, int*
   cfg.attrs = at;
   cfg.numAttrs = n_at;
   MIX_OP_CUDA(cudaLaunchKernelEx(&cfg, p.cluster ? expert_order_kernel<true> : expert_order_kernel<false>, idx, (int)n, n_experts,
-                                 static_cast<const int*>(hist), p.chunks, p.steps, offsets, order, position));
+                                 static_cast<const int*>(hist), p.chunks, p.steps, (int)p.scan, offsets, order, position));
   return MIX_OK;
 }

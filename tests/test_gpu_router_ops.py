@@ -258,3 +258,20 @@ def test_captured_with_rewritten_inputs_and_on_another_stream():
         seg.copy_(torch.tensor([0, cut, live], dtype=torch.int32))
         graph.replay()
         assert all(torch.equal(a, b) for a, b in zip(out, step()))
+
+
+def test_expert_order_of_many_entries():
+    """More entries than the host sorts in reasonable time: against a stable sort."""
+    for T, k, E in ((300000, 8, 512), (1 << 20, 16, 3)):
+        g = torch.Generator(device=DEV).manual_seed(E)
+        idx = torch.randint(-1, E, (T, k), generator=g, device=DEV, dtype=torch.int32)
+        offsets, order, position = mix.expert_order(idx, E)
+        key = torch.where(idx.view(-1) < 0, E, idx.view(-1)).long()
+        want = torch.sort(key, stable=True).indices
+        counts = torch.bincount(key, minlength=E + 1)
+        assert torch.equal(offsets.long(), torch.cat([torch.zeros_like(counts[:1]), counts[:E].cumsum(0)]))
+        n = int(offsets[-1])
+        assert torch.equal(order[:n].long(), want[:n]) and (order[n:] == -1).all()
+        place = torch.empty_like(want)
+        place[want] = torch.arange(T * k, device=DEV)
+        assert torch.equal(position.view(-1).long(), torch.where(key < E, place, -1))
