@@ -519,6 +519,7 @@ int mix_sae_apply_static(void* hidden, int n_rows, int d_model, const mix_sae_we
  * fails nothing has been enqueued, unless the code is MIX_ERR_CUDA.
  * Two calls with the same inputs give the same bits: nothing is added up in an order that depends on timing. */
 enum { MIX_DTYPE_F32 = 0, MIX_DTYPE_BF16 = 1, MIX_DTYPE_F16 = 2 };   /* element types of the tensors of these calls */
+#define MIX_OP_MAX_ROWS 1073741824         /* most rows (tokens) of a call, and most tiles of a product: beyond, OUT_OF_RANGE */
 #define MIX_ORDER_MAX_ENTRIES 16777216    /* mix_expert_order: most entries of a call */
 #define MIX_BALANCE_MAX_SEGMENTS 65536    /* mix_router_balance: most segments of a call */
 #define MIX_COMBINE_MAX_N 8388480         /* mix_expert_combine: widest row */
@@ -601,7 +602,7 @@ int mix_linear_int_grouped(const signed char* codes, const float* scale, int n_r
                           void* stream, char* errbuf, int errbuf_len);
 
 /* Copy the status word of the 8-bit products on the current device to *bits (host) and clear it: MIX_STATUS_WAIT_TIMEOUT after a bounded wait
-   inside a product kernel ran out, in which case the results since the last call are invalid.  Synchronises `stream`. */
+   inside a product kernel ran out, in which case the results since the last call are invalid.  Synchronises `stream`; not capturable. */
 int mix_linear_int_status(unsigned* bits, void* stream, char* errbuf, int errbuf_len);
 
 /* The experts' results summed over each token's experts: out[t, :] = sum_j weights[t, j] y[position[t, j], :], j rising, in fp32, rounded

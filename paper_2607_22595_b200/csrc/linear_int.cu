@@ -650,7 +650,10 @@ cudaError_t gemm_launch(const Gemm& g, const TilePlan& p, int dev, int n_sms, cu
 // 2500 + 60 n more where its parts have to meet.  Among the tile sizes the one is taken whose waves cost least.  (1000 x 5120 codes by
 // 9992 channels: five tiles of 200 tokens instead of four of 250, 4 waves' worth instead of 4.5: %s us, 42 before; 16 x 4096 by 4096
 // channels: in four parts %s us, %s in one.)
-// By experts the host knows the rows' average alone: tiles as large as an even share, in pairs above 128 tokens.
+// By experts the host knows the rows' average alone, and a tile costs little more than the tokens it has: tiles hold about twice an
+// even share, in pairs above 96.  (64 experts of 2048 x 2048, 32 rows each on average: 48.4 us with tiles of 32 tokens, 44.1 with 64;
+// 64 rows: 50.3 with 64, 45.5 with 128; 128 rows: 62.9 with 128, 55.2 in pairs.  8 experts of 4096 x 4096, 24 rows: 22.2 with 32, 24.7
+// with 64; 96 rows: 26.0 with 128, 26.9 in pairs.)
 TilePlan tile_plan(const Gemm& g, int n_sms) {
   const long long kbs = div_up(g.K, kKBytes);
   TilePlan best = {kSingle, 32, 32, 1};
@@ -674,8 +677,8 @@ TilePlan tile_plan(const Gemm& g, int n_sms) {
     return best;
   }
   const int even = (int)div_up(g.n_rows, g.E);
-  if (even > 128) return TilePlan{kPairs, 256, 256, 1};
-  const int nt = even <= 32 ? 32 : (even <= 64 ? 64 : 128);
+  if (even > 96) return TilePlan{kPairs, 256, 256, 1};
+  const int nt = even <= 24 ? 32 : (even <= 40 ? 64 : 128);
   for (int parts = 1; parts <= kMostParts; parts *= 2) consider(parts > 1 ? kSplit : kSingle, nt, nt, parts);
   return best;
 }
@@ -693,14 +696,14 @@ cudaError_t gemm_pick(const Gemm& g, int dev, int n_sms, cudaStream_t s) {
 
 int gemm_call(const Gemm& g, int dtype, void* stream, char* errbuf, int errbuf_len) {
   if (op_elem_size(dtype) == 0) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "dtype %d is no MIX_DTYPE_*", dtype);
-  if (g.n_rows < 0) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "n_rows %d is negative", g.n_rows);
+  if (g.n_rows < 0 || g.n_rows > kOpMaxRows) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "%d rows, outside [0, %d]", g.n_rows, kOpMaxRows);
   if (g.K < 16 || g.K > MIX_I8_MAX_K) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "K %d outside [16, %d]", g.K, MIX_I8_MAX_K);
   if (g.K % 16) MIX_OP_FAIL(MIX_ERR_UNSUPPORTED, "K %d is not a multiple of 16", g.K);
   if (g.N < 1) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "N %d is below 1", g.N);
   if (g.E < 1 || g.E > kOpMaxExperts) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "n_experts %d outside [1, %d]", g.E, kOpMaxExperts);
   if ((long long)g.E * g.N > 0x7fffff00ll) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "%lld rows of W", (long long)g.E * g.N);
   const long long tiles = ((long long)g.n_rows / 32 + g.E) * ((g.N + kTileCh - 1) / kTileCh);
-  if (tiles > 0x7fffffffll) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "n_rows %d x N %d has too many tiles", g.n_rows, g.N);
+  if (tiles > kOpMaxRows) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "n_rows %d x N %d has too many tiles", g.n_rows, g.N);
   if (g.ld_out < g.N) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "row stride %lld of the output is below N %d", g.ld_out, g.N);
   if (g.n_rows == 0) return MIX_OK;
   if (!g.codes || !g.scale || !g.w || !g.w_scale || !g.out) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "codes, scale, W, w_scale and out are required");
@@ -762,7 +765,7 @@ cudaError_t combine_launch(const void* y, long long ld_y, int y_rows, const floa
 extern "C" int mix_quantize_rows(const void* x, int dtype, long long ld, int x_rows, const int* order, int k, int n_rows, int d,
                                     signed char* codes, float* scale, void* stream, char* errbuf, int errbuf_len) {
   if (dtype != MIX_DTYPE_BF16 && dtype != MIX_DTYPE_F16) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "dtype %d is neither bf16 nor fp16", dtype);
-  if (n_rows < 0 || x_rows < 0) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "%d rows of %d", n_rows, x_rows);
+  if (n_rows < 0 || x_rows < 0 || n_rows > kOpMaxRows) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "%d rows of %d", n_rows, x_rows);
   if (d < 16 || d > MIX_I8_MAX_K) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "d %d outside [16, %d]", d, MIX_I8_MAX_K);
   if (d % 16) MIX_OP_FAIL(MIX_ERR_UNSUPPORTED, "d %d is not a multiple of 16", d);
   if (ld < d) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "row stride %lld is below d %d", ld, d);
@@ -802,7 +805,7 @@ extern "C" int mix_linear_int_status(unsigned* bits, void* stream, char* errbuf,
 extern "C" int mix_expert_combine(const void* y, int dtype, long long ld_y, int y_rows, const float* weights, const int* position, int T, int k,
                                   int N, void* out, long long ld_out, void* stream, char* errbuf, int errbuf_len) {
   if (op_elem_size(dtype) == 0) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "dtype %d is no MIX_DTYPE_*", dtype);
-  if (T < 0 || y_rows < 0) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "%d tokens, %d rows of y", T, y_rows);
+  if (T < 0 || y_rows < 0 || T > kOpMaxRows) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "%d tokens, %d rows of y", T, y_rows);
   if (k < 1 || k > kOpMaxTopk) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "k %d outside [1, %d]", k, kOpMaxTopk);
   if (N < 1 || N > MIX_COMBINE_MAX_N) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "N %d outside [1, %d]", N, MIX_COMBINE_MAX_N);
   if (ld_y < N || ld_out < N) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "row strides %lld, %lld below N %d", ld_y, ld_out, N);

@@ -230,6 +230,7 @@ constexpr float kLowTotal = 1e-20f;        // below it a row's sigmoids are take
 
 constexpr int kOpMaxExperts = 512;
 constexpr int kOpMaxTopk = 16;
+constexpr int kOpMaxRows = MIX_OP_MAX_ROWS;      // (row numbers and a grid's stride added to them stay in 31 bits)
 
 // Calls f(std::integral_constant<int, G>, std::integral_constant<int, V>) for the narrowest row layout that holds E columns.
 #define MIX_ROW_LAYOUT(E, CALL)        \

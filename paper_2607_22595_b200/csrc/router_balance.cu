@@ -448,7 +448,7 @@ int router_args(const void* logits, int dtype, long long ld, int T, int E, int k
 }
 
 extern "C" long long mix_router_balance_workspace(int T, int n_experts, int n_seg) {
-  if (T < 0 || n_experts < 1 || n_experts > kOpMaxExperts || n_seg < 1 || n_seg > MIX_BALANCE_MAX_SEGMENTS) return MIX_ERR_OUT_OF_RANGE;
+  if (T < 0 || T > kOpMaxRows || n_experts < 1 || n_experts > kOpMaxExperts || n_seg < 1 || n_seg > MIX_BALANCE_MAX_SEGMENTS) return MIX_ERR_OUT_OF_RANGE;
   int dev, n_sms;
   if (op_device(&dev, &n_sms) != cudaSuccess) {
     cudaGetLastError();

@@ -523,7 +523,7 @@ namespace mix {
 int router_args(const void* logits, int dtype, long long ld, int T, int E, int k, int act, char* errbuf, int errbuf_len) {
   if (op_elem_size(dtype) == 0) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "dtype %d is no MIX_DTYPE_*", dtype);
   if (act != MIX_ACT_SOFTMAX && act != MIX_ACT_SIGMOID) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "act %d is neither softmax nor sigmoid", act);
-  if (T < 0) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "T %d is negative", T);
+  if (T < 0 || T > kOpMaxRows) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "T %d outside [0, %d]", T, kOpMaxRows);
   if (E < 1 || E > kOpMaxExperts) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "n_experts %d outside [1, %d]", E, kOpMaxExperts);
   if (k < 1 || k > kOpMaxTopk || k > E) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "k %d outside [1, min(%d, n_experts)]", k, kOpMaxTopk);
   if (ld < E) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "row stride %lld is below n_experts %d", ld, E);

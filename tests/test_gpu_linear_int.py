@@ -1,4 +1,8 @@
 """Products in 8-bit integers with a scale per token and output channel, alone and by experts, against 64 bits."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -372,3 +376,58 @@ def test_a_stream_given_by_argument():
     side.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     assert torch.equal(codes.double(), R.codes_of(x)[0])
+
+
+def test_the_first_calls_of_a_process_may_be_captured():
+    """Nothing has to be called before a capture, nor in a warm-up."""
+    code = """
+import torch, paper_2607_22595_b200 as mix
+g = torch.Generator(device="cuda").manual_seed(1)
+logits = torch.randn((40, 8), generator=g, device="cuda")
+x = torch.randn((40, 64), generator=g, device="cuda").to(torch.bfloat16)
+W = torch.randint(-9, 9, (8, 48, 64), generator=g, device="cuda", dtype=torch.int8)
+ws = torch.ones((8, 48), device="cuda")
+def step():
+    idx, w = mix.router_topk(logits, 2)
+    offsets, order, position = mix.expert_order(idx, 8)
+    codes, scale = mix.quantize_rows(x, order=order, k=2)
+    y = mix.linear_int_grouped(codes, scale, W, ws, offsets)
+    loss, counts, mean_p, rows = mix.router_balance(logits, idx)
+    return mix.expert_combine(y, w, position), mix.linear_int(codes, scale, W[0], ws[0]), mix.router_balance_grad(logits, idx, counts, rows, loss)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    out = step()
+graph.replay()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(out, step()))
+assert mix.linear_int_status() == 0
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=120)
+    assert done.returncode == 0, done.stderr[-2000:]
+
+
+def test_refused_tensors():
+    codes, scale, W, w_scale = _operands(20, 64, 30, 1)
+    grouped = _operands(20, 64, 30, 1, E=2)
+    offsets = torch.tensor([0, 5, 20], dtype=torch.int32, device=DEV)
+    x = torch.zeros((4, 64), dtype=torch.bfloat16, device=DEV)
+    position = torch.zeros((4, 2), dtype=torch.int32, device=DEV)
+    for call in (lambda: mix.linear_int(codes.float(), scale, W, w_scale), lambda: mix.linear_int(codes, scale[:19], W, w_scale),
+                 lambda: mix.linear_int(codes, scale, W[:, :48], w_scale), lambda: mix.linear_int(codes, scale, W, w_scale.double()),
+                 lambda: mix.linear_int(codes, scale, W, w_scale, bias=w_scale[:5]), lambda: mix.linear_int(codes, scale, W, w_scale, dtype=torch.float64),
+                 lambda: mix.linear_int(codes, scale, W, w_scale, out=torch.empty((20, 31), device=DEV)), lambda: mix.linear_int(codes, scale, W, w_scale, dtype=3),
+                 lambda: mix.linear_int(codes, scale, grouped[2], grouped[3]), lambda: mix.linear_int_grouped(codes, scale, W, w_scale, offsets),
+                 lambda: mix.linear_int_grouped(codes, scale, grouped[2], grouped[3], None),
+                 lambda: mix.linear_int_grouped(codes, scale, grouped[2], grouped[3], offsets[:2]),
+                 lambda: mix.linear_int_grouped(codes, scale, grouped[2], grouped[3], offsets.long()),
+                 lambda: mix.quantize_rows(x, order=offsets.long()), lambda: mix.quantize_rows(x, order=offsets, k=0),
+                 lambda: mix.quantize_rows(x, codes=torch.empty((4, 64), device=DEV)), lambda: mix.expert_combine(x, torch.zeros((4, 3), device=DEV), position),
+                 lambda: mix.expert_combine(x, torch.zeros((4, 2), device=DEV), position, out=torch.empty((4, 64), device=DEV))):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: mix.quantize_rows(x.float()), lambda: mix.quantize_rows(x[:, :40].contiguous()),
+                 lambda: mix.linear_int(codes[:, :40].contiguous(), scale, W[:, :40].contiguous(), w_scale)):
+        with pytest.raises(mix.MixError):
+            call()

@@ -275,3 +275,43 @@ def test_expert_order_of_many_entries():
         place = torch.empty_like(want)
         place[want] = torch.arange(T * k, device=DEV)
         assert torch.equal(position.view(-1).long(), torch.where(key < E, place, -1))
+
+
+def test_no_rows():
+    x, none = torch.empty((0, 12), device=DEV), torch.empty((0, 3), dtype=torch.int32, device=DEV)
+    idx, w = mix.router_topk(x, 3)
+    assert idx.shape == (0, 3) and w.shape == (0, 3)
+    assert mix.router_topk_grad(x, idx, w, w).shape == (0, 12)
+    for seg in (None, torch.zeros(5, dtype=torch.int32, device=DEV)):
+        loss, counts, mean_p, rows = mix.router_balance(x, none, seg)
+        n = 1 if seg is None else 4
+        assert loss.shape == (n,) and not loss.any() and counts.shape == (n, 12) and not counts.any() and not mean_p.any() and not rows.any()
+        assert mix.router_balance_grad(x, none, counts, rows, torch.ones(n, device=DEV), seg).shape == (0, 12)
+
+
+def test_outputs_that_are_given_and_refused():
+    x = _logits(20, 16, "fp32", seed=1)
+    idx, w = torch.empty((20, 4), dtype=torch.int32, device=DEV), torch.empty((20, 4), device=DEV)
+    out = mix.router_topk(x, 4, idx=idx, weights=w)
+    assert out[0] is idx and out[1] is w
+    offsets, order, position = (torch.empty(s, dtype=torch.int32, device=DEV) for s in ((17,), (80,), (20, 4)))
+    got = mix.expert_order(idx, 16, offsets=offsets, order=order, position=position)
+    assert got[0] is offsets and got[1] is order and got[2] is position and offsets[-1] == (idx >= 0).sum()
+    long = idx.long()
+    for call in (lambda: mix.router_topk(x, 0), lambda: mix.router_topk(x, 17), lambda: mix.router_topk(x, 4, idx=idx[:, :3], weights=w),
+                 lambda: mix.router_topk(x, 4, idx=long, weights=w), lambda: mix.router_topk(x.double(), 4), lambda: mix.router_topk(x[0], 4),
+                 lambda: mix.router_topk(x.t(), 4), lambda: mix.router_topk(x, 4, n_live=torch.ones(2, dtype=torch.int32, device=DEV)),
+                 lambda: mix.router_topk(x, 4, act=7), lambda: mix.expert_order(long, 16), lambda: mix.expert_order(idx, 0),
+                 lambda: mix.expert_order(idx.t(), 16), lambda: mix.router_topk_grad(x, idx, w, w.double()),
+                 lambda: mix.router_topk_grad(x, idx, w, w, d_logits=torch.empty_like(x, dtype=torch.bfloat16)),
+                 lambda: mix.router_balance(x, long), lambda: mix.router_balance(x, idx, torch.zeros(1, dtype=torch.int32, device=DEV)),
+                 lambda: mix.router_balance(x, idx, torch.zeros(3, device=DEV)), lambda: mix.router_balance(x[:19], idx)):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(mix.MixError) as e:
+        mix.router_topk(torch.zeros((4, 600), device=DEV), 2)
+    assert e.value.code == -2 and "n_experts" in str(e.value)
+    with pytest.raises(mix.MixError):
+        mix.router_topk(x[:1].expand(20, 16), 4)           # rows that lie on top of each other
+    with pytest.raises(mix.MixError):
+        mix.router_topk(x, 4, act=mix.MIX_ACT_NONE)

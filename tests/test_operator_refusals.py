@@ -17,7 +17,9 @@ FN = dict(topk="mix_router_topk", topk_grad="mix_router_topk_grad", order="mix_e
           balance_grad="mix_router_balance_grad", quantize="mix_quantize_rows", linear="mix_linear_int", grouped="mix_linear_int_grouped",
           combine="mix_expert_combine")
 REFUSED = [
-    ("topk", {0: None}, INVALID), ("topk", {1: 3}, INVALID), ("topk", {2: 7}, RANGE), ("topk", {3: -1}, RANGE), ("topk", {4: 0}, RANGE),
+    ("topk", {0: None}, INVALID), ("topk", {1: 3}, INVALID), ("topk", {2: 7}, RANGE), ("topk", {3: -1}, RANGE), ("topk", {3: (1 << 30) + 1}, RANGE), ("balance", {4: (1 << 30) + 1}, RANGE),
+    ("linear", {2: (1 << 30) + 1}, RANGE), ("linear", {2: 1 << 30, 6: 1 << 20, 10: 1 << 20}, RANGE), ("quantize", {6: (1 << 30) + 1, 3: (1 << 30) + 1}, RANGE),
+    ("combine", {6: (1 << 30) + 1}, RANGE), ("topk", {4: 0}, RANGE),
     ("topk", {4: 513, 2: 513}, RANGE), ("topk", {5: 0}, RANGE), ("topk", {5: 9}, RANGE), ("topk", {5: 17, 4: 64, 2: 64}, RANGE), ("topk", {6: 2}, INVALID),
     ("topk", {9: None}, INVALID), ("topk", {10: None}, INVALID),
     ("topk_grad", {0: None}, INVALID), ("topk_grad", {12: 7}, RANGE), ("topk_grad", {11: None}, INVALID), ("topk_grad", {8: None}, INVALID),
