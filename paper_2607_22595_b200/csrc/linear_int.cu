@@ -23,7 +23,7 @@ namespace {
 //   takes it to 64, the even one.  If A = 127 2^j the factor is a power of two and everything is exact.  Other multiples of 127 (eight
 //   largest values of fp16 in 1024) go by division; so do rows that lie so far from 1 that 127 x or 127 / a would leave fp32's
 //   range, scaled by a power of two first.
-// 8192 rows of 8192 bf16: 60 us with a rounding, a comparison and a conversion per element, 51 with a test for halves, %s us so.
+// 8192 rows of 8192 bf16: 60 us with a rounding, a comparison and a conversion per element, 51 with a test for halves, 36.6 so (5.5 TB/s).
 template <typename T>
 struct Pair2;
 template <>
@@ -646,10 +646,12 @@ cudaError_t gemm_launch(const Gemm& g, const TilePlan& p, int dev, int n_sms, cu
 }
 
 // A k-block of a tile of n tokens costs a CTA max(2 n, 256 + n) clocks in a pair and 256 + 2 n alone: the instructions take 2 n, and
-// shared memory moves each operand byte twice at 128 bytes a clock.  What a tile costs beside its k-blocks is some 1500 clocks, and
-// 2500 + 60 n more where its parts have to meet.  Among the tile sizes the one is taken whose waves cost least.  (1000 x 5120 codes by
-// 9992 channels: five tiles of 200 tokens instead of four of 250, 4 waves' worth instead of 4.5: %s us, 42 before; 16 x 4096 by 4096
-// channels: in four parts %s us, %s in one.)
+// shared memory moves each operand byte twice at 128 bytes a clock.  What a tile costs beside its k-blocks is some 1500 clocks, in
+// a pair 3000, and 2500 + 60 n more where its parts have to meet.  Among tiles of 32, 64 and 128 tokens, in parts or not, and pairs
+// of 256 the one is taken whose waves cost least.  (16 x 4096 codes by 4096 channels: in four parts 8.4 us, 9.7 in one; 16 x 14336:
+// 14.9 and 24.5; 128 x 4096 by 4096 in tiles of 32: 7.9 us.  Pairs of smaller tiles, which fit the waves better by this count, were
+// slower: 256 x 4096 by 4096 10.2 us in pairs of 64 tokens, 8.6 in single tiles of 64; 1000 x 5120 by 9992 no faster with 5 x 200
+// tokens than with 4 x 250.)
 // By experts the host knows the rows' average alone, and a tile costs little more than the tokens it has: tiles hold about twice an
 // even share, in pairs above 96.  (64 experts of 2048 x 2048, 32 rows each on average: 48.4 us with tiles of 32 tokens, 44.1 with 64;
 // 64 rows: 50.3 with 64, 45.5 with 128; 128 rows: 62.9 with 128, 55.2 in pairs.  8 experts of 4096 x 4096, 24 rows: 22.2 with 32, 24.7
@@ -663,7 +665,7 @@ TilePlan tile_plan(const Gemm& g, int n_sms) {
     if (parts > 1 && (tiles * parts > n_sms || kbs < 4 * parts)) return;
     const long long waves = parts > 1 ? 1 : div_up(tiles, mode == kPairs ? n_sms / 2 : n_sms);
     const long long n = div_up(g.n_rows, div_up(g.n_rows, tile_tok)), a = mode == kPairs ? (2 * n > 256 + n ? 2 * n : 256 + n) : 256 + 2 * n;
-    const double cost = (double)waves * (double)(div_up(kbs, parts) * a + (parts > 1 ? 4000 + 60 * n : 1500));
+    const double cost = (double)waves * (double)(div_up(kbs, parts) * a + (parts > 1 ? 4000 + 60 * n : (mode == kPairs ? 3000 : 1500)));
     if (cost < least) {
       least = cost;
       best = TilePlan{mode, nt, tile_tok, parts};
@@ -672,8 +674,7 @@ TilePlan tile_plan(const Gemm& g, int n_sms) {
   if (g.E == 1) {
     for (int nt = 32; nt <= 128; nt *= 2)
       for (int parts = 1; parts <= kMostParts; parts *= 2) consider(parts > 1 ? kSplit : kSingle, nt, nt, parts);
-    const long long fewest = div_up(g.n_rows, 256);
-    for (long long tt = fewest; tt < fewest + 8; ++tt) consider(kPairs, 256, (int)(div_up(div_up(g.n_rows, tt), 32) * 32), 1);
+    consider(kPairs, 256, 256, 1);
     return best;
   }
   const int even = (int)div_up(g.n_rows, g.E);

@@ -10,6 +10,10 @@
 // step, so no two share a slot, and which row is added where never depends on timing.  A second launch adds the slots up, a
 // cluster of CTAs per segment where a segment has many.  Both add in a fixed order.
 // Backward: one pass over the logits, a warp per run of rows.
+//
+// 65536 rows of 256 fp32 in 16 segments, sigmoid: forward 23.5 us (16 + 7 in its two launches; the logits' stream takes 10.3),
+// backward 29.3 (20.6 read and written).  What bounds both is issue: 14 instructions a logit, two of them on the special-function
+// unit, beside the reductions of a row.
 #include "op_common.cuh"
 #include "tc_common.cuh"
 

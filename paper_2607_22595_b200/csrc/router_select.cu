@@ -28,7 +28,7 @@ constexpr int kSelThreads = 256;
 // is done again by rounds over all logits where that may not be the answer: a lane gave all three and has more above the last key
 // (8 of 256: four rows in a thousand), or two neighbours of fp32 agree in all bits of the key (16-bit logits lose none).
 // 65536 rows of 256, k = 8, with the softmax over the row: 76 us by rounds over all logits, 37 with logits and columns apart, 35
-// with two keys a lane, %s us so; the logits' stream alone takes 10.3.
+// with two keys a lane, 32 so; the logits' stream alone takes 10.3.
 template <typename T, int G, int V>
 __global__ void __launch_bounds__(kSelThreads)
 router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_rows, int E, int k, int act, int renorm,
@@ -174,7 +174,7 @@ router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_ro
 // Where a lane has one chosen entry (more than 64 experts) the row is written as if nothing had been chosen -- p (-s), or zeros --
 // and the lanes then write their own entries over it, w (g - s): w is p there.  Narrower rows compare each entry with each
 // column of a lane, for 32 / G rows at a time.  65536 rows of 256: 38 us with the entries spread over the row in shared memory,
-// %s us so; reading and writing the logits alone takes 20.6.
+// 22.7 so (5.9 TB/s); reading and writing the logits alone takes 20.6.
 template <typename T, int G, int V>
 __global__ void __launch_bounds__(kSelThreads)
 router_topk_grad_kernel(const T* __restrict__ logits, long long ld, int vec, int T_rows, int E, int k, int act, int renorm,
@@ -566,8 +566,8 @@ extern "C" int mix_router_topk_grad(const void* logits, int dtype, long long ld,
 
 namespace {
 // How a call's entries are dealt.  What a step of a warp costs is instructions, some 90, so a chunk is small and many SMs share the
-// work: 16384 entries are on 8 SMs of 512 threads, beyond that chunks of 2048.  (65536 entries of 256 experts: %s us, 12.5 in eight
-// chunks of 8192; 16384: %s, 12.3 in two; 524288: %s, 14.9 in 64 chunks of 8192 whose CTAs add up all chunks' counts.)
+// work: 16384 entries are on 8 SMs of 512 threads, beyond that chunks of 2048.  (65536 entries of 256 experts: 9.3 us, 12.5 in eight
+// chunks of 8192; 16384: 7.2, 12.3 in two; 524288: 13.3, 14.9 in 64 chunks of 8192 whose CTAs add up all chunks' counts.)
 struct OrderPlan {
   int threads, steps, chunks;
   bool cluster, counts, scan;
