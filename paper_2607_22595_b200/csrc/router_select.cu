@@ -21,14 +21,22 @@ constexpr int kSelThreads = 256;
 // ---------------------------------------------------------------------------------------------------- selection
 // The selection compares the logits themselves, never probabilities: those round, and two logits that differ could tie.
 //
-// Rows of up to 128 experts: k rounds of an arg-max over the G lanes, 32 / G rows of a warp side by side.
-// Wider rows (a warp each) are bound by comparisons and selections, which issue at half rate, so they compare keys that carry the
-// column: the logit's order-preserving bits, the lowest 8 or 9 replaced by ~column.  No two are equal, a round is one reduction
-// over the warp, and a lane keeps its three largest keys; one that has given its first offers its second.  k + 1 rounds.  The row
-// is done again by rounds over all logits where that may not be the answer: a lane gave all three and has more above the last key
-// (8 of 256: four rows in a thousand), or two neighbours of fp32 agree in all bits of the key (16-bit logits lose none).
-// 65536 rows of 256, k = 8, with the softmax over the row: 76 us by rounds over all logits, 37 with logits and columns apart, 35
-// with two keys a lane, 32 so; the logits' stream alone takes 10.3.
+// What bounds it is comparisons and selections, which issue at half rate, so it compares keys that carry the column: the logit's
+// order-preserving bits, the lowest 3 to 9 replaced by ~column.  No two keys of a row are equal, and a round is one reduction over
+// the G lanes.  fp32 logits lose bits by that: where two neighbours among the first k + 1 agree in what is left, the row is done
+// again by rounds that compare logits and columns (16-bit logits lose none).
+// Rows of up to 64 experts: k rounds over all keys, 32 / G rows of a warp side by side.
+// Wider rows: a lane keeps its three largest keys; one that has given its first offers its second.  Where a lane gave all three and
+// has more above the last key (8 of 256: four rows in a thousand) the row is done again too.
+// 65536 rows of 256, k = 8, with the softmax over the row: 76 us by rounds over logits, 35 with two keys a lane, 32 with three and a
+// look at each round's key, 29.8 so; the logits' stream alone takes 10.3.
+template <int G>
+__device__ __forceinline__ unsigned group_max_key(unsigned x) {
+  if (G == 32) return __reduce_max_sync(0xffffffffu, x);
+#pragma unroll
+  for (int o = 1; o < G; o <<= 1) x = max(x, __shfl_xor_sync(0xffffffffu, x, o));
+  return x;
+}
 template <typename T, int G, int V>
 __global__ void __launch_bounds__(kSelThreads)
 router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_rows, int E, int k, int act, int renorm,
@@ -53,23 +61,22 @@ router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_ro
 #pragma unroll
     for (int v = 0; v < V; ++v) x[v] = fmaxf(x[v], -INFINITY);             // (the larger of a NaN and a number is the number)
   }
-  float top = 0.f;
-  if (G < 32) top = group_max<G>(top_of<V>(x));
-  int my_idx[S];
-  float my_x[S];
+  constexpr unsigned kCol = G * V - 1;                                     // the key's bits that hold ~column
+  constexpr unsigned kNone = 0x007fffffu & ~kCol;                          // -inf's key
+  constexpr int kRounds = G == 1 ? 8 : kOpMaxTopk;
+  static_assert((kCol & G * V) == 0, "a power of two");
+  unsigned key[V], mine[S];
 #pragma unroll
-  for (int s = 0; s < S; ++s) { my_idx[s] = -1; my_x[s] = -INFINITY; }
-  bool rounds = true;
-  if (G == 32) {
-    constexpr unsigned kCol = V * 32 - 1;                                  // the key's bits that hold ~column
-    constexpr unsigned kNone = 0x007fffffu & ~kCol;                        // -inf's key
-    static_assert((kCol & V * 32) == 0, "a power of two");
-    unsigned key[V], k1[V / 2], k2[V / 2], k3[V / 4];                      // sorted parts of the lane's keys, their three largest
+  for (int v = 0; v < V; ++v) {
+    const unsigned bits = __float_as_uint(x[v] + 0.f);                     // -0 and 0 are equal
+    key[v] = ((bits ^ ((unsigned)((int)bits >> 31) | 0x80000000u)) & ~kCol) | (kCol - (unsigned)row_col<T, G>(v, sub));
+  }
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const unsigned bits = __float_as_uint(x[v] + 0.f);                   // -0 and 0 are equal
-      key[v] = ((bits ^ ((unsigned)((int)bits >> 31) | 0x80000000u)) & ~kCol) | (kCol - (unsigned)row_col<T, G>(v, sub));
-    }
+  for (int s = 0; s < S; ++s) mine[s] = 0u;
+  const int n_rounds = sizeof(T) == 4 ? k + 1 : k;
+  bool unsure = false;
+  if (S == 1) {
+    unsigned k1[V / 2], k2[V / 2], k3[V / 4];                              // sorted parts of the lane's keys, their three largest
 #pragma unroll
     for (int i = 0; i < V / 2; ++i) {
       k1[i] = max(key[2 * i], key[2 * i + 1]);
@@ -85,49 +92,63 @@ router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_ro
         k3[i] = n == V / 4 ? min(m, l) : max(min(m, l), max(k3[i], k3[i + n]));
       }
     }
-    unsigned first = k1[0], second = k2[0], third = k3[0], last = 0u, mine = 0u;
-    int given = 0;
+    unsigned first = k1[0], second = k2[0], third = k3[0], last = 0u;
 #pragma unroll
-    for (int j = 0; j < kOpMaxTopk + 1; ++j) {
-      if (j > k) break;
-      last = __reduce_max_sync(0xffffffffu, first);
-      if ((last & ~kCol) <= kNone) break;                                  // nothing but -inf on offer
-      mine = j == sub ? last : mine;
-      if (first == last) {
-        first = second;
-        second = third;
-        third = 0u;
-        ++given;
-      }
+    for (int j = 0; j < kRounds + 1; ++j) {
+      if (j >= n_rounds) break;
+      last = group_max_key<G>(first);
+      mine[0] = j == sub ? last : mine[0];
+      const bool mine_goes = first == last;
+      first = mine_goes ? second : first;
+      second = mine_goes ? third : second;
+      third = mine_goes ? 0u : third;
     }
-    bool unsure = false;
-    if (__any_sync(0xffffffffu, given > 2)) {
-      last = max(last, kNone + kCol + 1u);
+    if (__any_sync(0xffffffffu, first == 0u)) {                            // a lane gave all three
       int above = 0;
 #pragma unroll
       for (int v = 0; v < V; ++v) above += key[v] >= last;
-      unsure = above != given;
+      unsure = first == 0u && above > 3;
     }
-    const unsigned after = __shfl_down_sync(0xffffffffu, mine, 1);         // (by all lanes)
-    if (sizeof(T) == 4) unsure |= sub < k && mine != 0u && ((after ^ mine) & ~kCol) == 0u;
-    rounds = __any_sync(0xffffffffu, unsure);
-    if (!rounds && sub < k && mine != 0u) {
-      my_idx[0] = (int)(kCol - (mine & kCol));
-      // (the bits that gave way to the column were 0 in a 16-bit logit, 1 in the key of a negative one)
-      my_x[0] = sizeof(T) == 4 ? to_f32(logits[t * ld + my_idx[0]]) : key2f((mine & 0x80000000u) ? mine & ~kCol : mine | kCol);
+    const unsigned after = __shfl_down_sync(0xffffffffu, mine[0], 1, G);   // (by all lanes)
+    if (sizeof(T) == 4) unsure |= sub < k && sub < G - 1 && (mine[0] & ~kCol) > kNone && ((after ^ mine[0]) & ~kCol) == 0u;
+  } else {
+    unsigned before = 0u;
+#pragma unroll
+    for (int j = 0; j < kRounds + 1; ++j) {
+      if (j >= n_rounds) break;
+      unsigned m = key[0];
+#pragma unroll
+      for (int v = 1; v < V; ++v) m = max(m, key[v]);
+      m = group_max_key<G>(m);
+      if (j < kRounds && j % G == sub) mine[j < kRounds ? j / G : 0] = m;
+      if (sizeof(T) == 4) unsure |= (m & ~kCol) > kNone && ((m ^ before) & ~kCol) == 0u;
+      before = m;
+#pragma unroll
+      for (int v = 0; v < V; ++v) key[v] = key[v] == m ? 0u : key[v];
     }
   }
+  const bool rounds = __any_sync(0xffffffffu, unsure);
+  int my_idx[S];
+  float my_x[S];
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+    const bool some = !rounds && s * G + sub < k && (mine[s] & ~kCol) > kNone;
+    my_idx[s] = some ? (int)(kCol - (mine[s] & kCol)) : -1;
+    my_x[s] = -INFINITY;
+    // (the bits that gave way to the column were 0 in a 16-bit logit, 1 in the key of a negative one)
+    if (some) my_x[s] = sizeof(T) == 4 ? to_f32(logits[t * ld + my_idx[s]]) : key2f((mine[s] & 0x80000000u) ? mine[s] & ~kCol : mine[s] | kCol);
+  }
   if (rounds) {
-    float key[V];
+    float left[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) key[v] = x[v];
+    for (int v = 0; v < V; ++v) left[v] = x[v];
 #pragma unroll
-    for (int j = 0; j < (G == 1 ? 8 : kOpMaxTopk); ++j) {
+    for (int j = 0; j < kRounds; ++j) {
       if (j >= k) break;
-      const float m = group_max<G>(top_of<V>(key));
+      const float m = group_max<G>(top_of<V>(left));
       unsigned c = 0xffffffffu;
 #pragma unroll
-      for (int v = V - 1; v >= 0; --v) c = key[v] == m ? (unsigned)row_col<T, G>(v, sub) : c;   // (columns rise with v)
+      for (int v = V - 1; v >= 0; --v) c = left[v] == m ? (unsigned)row_col<T, G>(v, sub) : c;   // (columns rise with v)
       if (G == 32) {
         c = __reduce_min_sync(0xffffffffu, c);
       } else {
@@ -135,14 +156,14 @@ router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_ro
         for (int o = 1; o < G; o <<= 1) c = min(c, __shfl_xor_sync(0xffffffffu, c, o));
       }
 #pragma unroll
-      for (int v = 0; v < V; ++v) key[v] = (unsigned)row_col<T, G>(v, sub) == c ? -INFINITY : key[v];
+      for (int v = 0; v < V; ++v) left[v] = (unsigned)row_col<T, G>(v, sub) == c ? -INFINITY : left[v];
       if (j % G == sub && m > -INFINITY) {
         my_idx[j / G] = (int)c;
         my_x[j / G] = m;
       }
     }
   }
-  if (G == 32) top = __shfl_sync(0xffffffffu, my_x[0], 0);                 // the first one chosen
+  const float top = __shfl_sync(0xffffffffu, my_x[0], 0, G);               // the first one chosen
   const bool plain = act == MIX_ACT_SIGMOID && !renorm;                    // the weight is the sigmoid itself
   float total = 0.f;
   if (act == MIX_ACT_SOFTMAX && !renorm) total = scores<V>(act, top, false, x);
