@@ -173,13 +173,13 @@ router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_ro
     if (renorm) total += my_x[s];
   }
   if (!plain) total = group_sum<G>(total);
-  const float by = plain ? 1.f : rcp_hw(total);
+  const float norm = plain ? 1.f : total;                                  // (divided: the weight of a single one chosen is 1 and its gradient 0)
 #pragma unroll
   for (int s = 0; s < S; ++s) {
     const int j = s * G + sub;
     if (j < k && t < T_rows) {
       idx[t * k + j] = my_idx[s];
-      weights[t * k + j] = my_idx[s] >= 0 ? my_x[s] * by : 0.f;
+      weights[t * k + j] = my_idx[s] >= 0 ? __fdiv_rn(my_x[s], norm) : 0.f;
     }
   }
 }

@@ -315,3 +315,12 @@ def test_outputs_that_are_given_and_refused():
         mix.router_topk(x[:1].expand(20, 16), 4)           # rows that lie on top of each other
     with pytest.raises(mix.MixError):
         mix.router_topk(x, 4, act=mix.MIX_ACT_NONE)
+
+
+@pytest.mark.parametrize("act", ["softmax", "sigmoid"])
+def test_a_single_chosen_expert_has_weight_one_and_no_gradient(act):
+    for E in (1, 5, 64, 100, 300):
+        x = _logits(200, E, "fp32", seed=E, special=False, spread=4.0)
+        idx, w = mix.router_topk(x, 1, act=ACT[act])
+        assert (w == 1).all()
+        assert not mix.router_topk_grad(x, idx, w, torch.randn((200, 1), device=DEV), act=ACT[act]).any()
