@@ -321,15 +321,25 @@ balance_grad_kernel(const T* __restrict__ logits, long long ld, int vec, const i
     float coef = 0.f;
     if (a < b) {
       long long total = 0;
+      int c[V], most = 0;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const int c = row_col<T, G>(v, sub);
-        const int n = c < E ? counts[(size_t)s * E + c] : 0;
-        f[v] = (float)n;
-        total += n;
+        const int col = row_col<T, G>(v, sub);
+        c[v] = col < E ? counts[(size_t)s * E + col] : 0;
+        total += c[v];
+        most = max(most, c[v]);
       }
 #pragma unroll
-      for (int o = 1; o < G; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+      for (int o = 1; o < G; o <<= 1) {
+        total += __shfl_xor_sync(0xffffffffu, total, o);
+        most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+      }
+      // Where the experts are chosen nearly alike the largest share is taken off all of them, in whole numbers -- f_j - sum f p is the
+      // same, p adds up to 1 -- so that small differences are not those of large terms (and nothing is left where all are alike).
+      // Where few are chosen the shares stay: most of them are 0.
+      const int off = 2 * total > (long long)E * most ? most : 0;
+#pragma unroll
+      for (int v = 0; v < V; ++v) f[v] = (float)(c[v] - off);
       const int n = rows[s];
       coef = n > 0 ? d_loss[s] * (float)E / (float)n : 0.f;
       const float inv = total > 0 ? 1.f / (float)total : 0.f;

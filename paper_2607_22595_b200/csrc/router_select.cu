@@ -109,8 +109,9 @@ router_topk_kernel(const T* __restrict__ logits, long long ld, int vec, int T_ro
       for (int v = 0; v < V; ++v) above += key[v] >= last;
       unsure = first == 0u && above > 3;
     }
-    const unsigned after = __shfl_down_sync(0xffffffffu, mine[0], 1, G);   // (by all lanes)
-    if (sizeof(T) == 4) unsure |= sub < k && sub < G - 1 && (mine[0] & ~kCol) > kNone && ((after ^ mine[0]) & ~kCol) == 0u;
+    unsigned after = __shfl_down_sync(0xffffffffu, mine[0], 1, G);         // (by all lanes)
+    if (sub == k - 1) after = last;                                        // of the round behind the last one chosen
+    if (sizeof(T) == 4) unsure |= sub < k && (mine[0] & ~kCol) > kNone && ((after ^ mine[0]) & ~kCol) == 0u;
   } else {
     unsigned before = 0u;
 #pragma unroll

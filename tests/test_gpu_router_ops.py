@@ -324,3 +324,44 @@ def test_a_single_chosen_expert_has_weight_one_and_no_gradient(act):
         idx, w = mix.router_topk(x, 1, act=ACT[act])
         assert (w == 1).all()
         assert not mix.router_topk_grad(x, idx, w, torch.randn((200, 1), device=DEV), act=ACT[act]).any()
+
+
+def test_balance_gradient_is_zero_where_all_experts_are_chosen_alike():
+    for T, E in ((1, 2), (30, 3), (400, 7), (50, 16)):
+        x = _logits(T, E, "fp32", seed=E, special=False)
+        idx = torch.arange(E, dtype=torch.int32, device=DEV).repeat(T, 1)
+        for act in ("softmax", "sigmoid"):
+            loss, counts, mean_p, rows = mix.router_balance(x, idx, act=ACT[act])
+            R.within(loss, torch.ones_like(loss), (R.rel_p(x, act) + 72 * R.U) * torch.ones(1, device=DEV))
+            assert not mix.router_balance_grad(x, idx, counts, rows, loss, act=ACT[act]).any()
+
+
+def test_balance_gradient_of_nearly_even_shares():
+    """All but one of eight experts chosen: what is left of the shares is small, and still right to fp32's precision."""
+    x = _logits(1, 8, "fp32", seed=3, special=False, spread=3.0)
+    idx, _ = mix.router_topk(x, 7)
+    loss, counts, _, rows = mix.router_balance(x, idx)
+    one = torch.ones(1)
+    d = mix.router_balance_grad(x, idx, counts, rows, one.to(DEV))
+    ref, _ = R.balance_grad(x.cpu().double(), idx.cpu().long(), [0, 1], "softmax", one)
+    # f_j - f_max is 0 or -1 / 7, each entry a product of two probabilities (or p (1 - p)), with the same relative bound twice
+    p = R.probabilities(x.cpu().double(), "softmax")
+    out = p.argmin()
+    terms = p * p[0, out]
+    terms[0, out] = p[0, out] * (1 + p[0, out])
+    R.within(d.cpu(), ref, (2 * R.rel_p(x, "softmax") + 24 * R.U) * 8 / 7 * terms)
+
+
+@pytest.mark.parametrize("E", [3, 8, 9, 16, 17, 33, 64, 65, 80, 128, 129, 200, 256, 300, 512])
+def test_logits_that_differ_in_their_last_bits(E):
+    """fp32 logits a few steps apart, chosen and not chosen ones among them, below and above 0, at every k."""
+    T = 400
+    g = torch.Generator().manual_seed(E)
+    steps = torch.stack([torch.randperm(4 * E, generator=g)[:E] for _ in range(T)]).double()
+    x = (1.0 + steps * 2.0**-23) * torch.where(torch.rand((T, 1), generator=g) < 0.5, -1.0, 1.0).double()
+    few = torch.rand((T, E), generator=g) < 0.7               # in half of the rows only a few are close to each other
+    x = torch.where(few & (torch.arange(T)[:, None] % 2 == 0), x * 2.0 ** torch.randint(-3, 3, (T, E), generator=g), x).float()
+    want = torch.sort(x.double(), dim=1, descending=True, stable=True).indices
+    for k in sorted({1, 2, min(8, E), min(15, E), min(16, E)}):
+        idx, _ = mix.router_topk(x.to(DEV), k)
+        assert torch.equal(idx.cpu().long(), want[:, :k]), k
