@@ -139,17 +139,24 @@ __device__ __forceinline__ bool group_any(bool yes) {
   return G == 32 ? votes != 0u : ((votes >> first) & ((1u << (G & 31)) - 1u)) != 0u;
 }
 
-// e^x as 2^(x log2 e), log2 e in two parts: the argument is off by half a step of itself and no more, so the result by
-// |x| 2^-24 relative and the two steps of the hardware's 2^x.  expf takes twice as many instructions to save the first part, and a
-// logit's distance from the row's largest is rounded by as much already.  Results below 2^-126 are 0.
+// e^x as 2^(x log2 e) by the hardware's 2^x: the argument is off by half a step of itself (|x| U, U = 2^-24) and by what log2 e is off
+// (0.22 |x| U), the result by two steps (4 U).  expf takes seven instructions to save the first; a logit's distance from the row's
+// largest is rounded by as much already.  Results below 2^-126 are 0.
 __device__ __forceinline__ float exp2_hw(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-constexpr float kLog2eHi = 1.44269502162933350f, kLog2eLo = 1.92596299112661746e-8f;
-__device__ __forceinline__ float times_log2e(float x) { return fmaf(x, kLog2eHi, x * kLog2eLo); }      // (-inf stays -inf)
-__device__ __forceinline__ float exp_row(float x) { return exp2_hw(times_log2e(x)); }
+constexpr float kLog2e = 1.44269502162933350f;
+__device__ __forceinline__ float exp_row(float x) { return exp2_hw(x * kLog2e); }
+// e^(x - top), with top log2 e at hand: one multiply-add, which rounds once.  What the rounding of top log2 e is off is a factor that
+// all logits of the row have in common.  (Sizes above 10^38, where it would leave fp32's range, are subtracted first.)
+struct ExpFrom {
+  float top, scaled;
+  bool large;
+  __device__ __forceinline__ explicit ExpFrom(float t) : top(t), scaled(t * kLog2e), large(fabsf(t) > 1e38f) {}
+  __device__ __forceinline__ float operator()(float x) const { return large ? exp_row(x - top) : exp2_hw(fmaf(x, kLog2e, -scaled)); }
+};
 __device__ __forceinline__ float rcp_hw(float x) {
   float y;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -167,8 +174,8 @@ __device__ __forceinline__ float top_of(const float (&x)[V]) {             // (t
 // The score of one logit in a row whose largest is `top`; see scores().
 __device__ __forceinline__ float score(int act, float x, float top) {
   if (x == -INFINITY) return 0.f;
-  if (act == MIX_ACT_SOFTMAX) return x == top ? 1.f : exp_row(x - top);
-  return top >= 0.f ? sigmoid_row(x) : exp_row(x - top) * rcp_hw(1.f + exp_row(x));
+  if (act == MIX_ACT_SOFTMAX) return top == INFINITY ? (x == top ? 1.f : 0.f) : ExpFrom(top)(x);
+  return top >= 0.f ? sigmoid_row(x) : ExpFrom(top)(x) * rcp_hw(1.f + exp_row(x));
 }
 // Unnormalised scores of a lane's logits, in place, and their sum.  A NaN scores 0: one that is there makes the sum a NaN, which is
 // looked at once for all V.
@@ -188,9 +195,10 @@ __device__ __forceinline__ float scores(int act, float top, bool low, float (&x)
     } else if (top == -INFINITY) {
       top = 0.f;
     }
+    const ExpFrom e(top);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      x[v] = exp_row(x[v] - top);
+      x[v] = e(x[v]);
       if (slope) (*slope)[v] = x[v];
       total += x[v];
     }
@@ -204,9 +212,10 @@ __device__ __forceinline__ float scores(int act, float top, bool low, float (&x)
     }
   } else {
     const float off = top < 0.f && top > -INFINITY ? top : 0.f;
+    const ExpFrom e(off);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const float r = rcp_hw(1.f + exp_row(x[v])), s = off == 0.f ? sigmoid_row(x[v]) : exp_row(x[v] - off) * r;
+      const float r = rcp_hw(1.f + exp_row(x[v])), s = off == 0.f ? sigmoid_row(x[v]) : e(x[v]) * r;
       if (slope) (*slope)[v] = s * r;
       x[v] = s;
       total += s;

@@ -139,10 +139,11 @@ def reach(x):
 
 
 def rel_p(x, act):
-    """Relative bound on a probability.  e^d, d = x - top: the difference and the exponent's argument are off by half a step of d
-    each and the exponential by two steps, (2 |d| + 4) U.  The sum of up to 512 such terms is off by their mean, weighted by p --
-    sum p |d| is at most the entropy, ln 512 < 6.3 -- that is 17 U, and by 24 U of additions (a tree behind 16 serial ones);
-    reciprocal and products 4 U.  A sigmoid's own steps (an addition and a reciprocal, 3 U) stand in the place of the difference's."""
+    """Relative bound on a probability.  e^d, d = x - top, is a power of 2 whose argument is off by half a step of d and by what log2 e
+    is off, or, of sizes beyond 10^38, by half a step of d twice; two steps of the power itself: (2 |d| + 4) U at most.  The sum of up
+    to 512 such terms is off by their mean, weighted by p -- sum p |d| is at most the entropy, ln 512 < 6.3 -- that is 17 U, and by 24 U
+    of additions (a tree behind 16 serial ones); reciprocal and products 4 U.  A sigmoid's own steps (an addition and a reciprocal,
+    3 U) stand in the place of the difference's."""
     return (2 * (reach(x) + 8) + 32) * U
 
 
