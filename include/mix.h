@@ -613,6 +613,15 @@ int mix_linear_int_status(unsigned* bits, void* stream, char* errbuf, int errbuf
 int mix_expert_combine(const void* y, int dtype, long long ld_y, int y_rows, const float* weights, const int* position, int T, int k, int N,
                        void* out, long long ld_out, void* stream, char* errbuf, int errbuf_len);
 
+/* Gradients of that sum for d_out (dtype [T, N], rows ld_d apart): d_weights fp32 [T, k] = <d_out[t, :], y[position[t, j], :]>, 0 for entries that
+   name no row -- with mix_router_topk_grad() the way from a loss back to the (steered) logits -- and, where d_y (dtype [y_rows, N], rows ld_dy
+   apart) is not NULL, d_y[position[t, j], :] = weights[t, j] d_out[t, :].  Rows that no entry names are left as they were; a row of y may be
+   named once only where d_y is wanted, as in mix_expert_order()'s position.  weights may be NULL without d_y.
+   Errors: as mix_expert_combine(). */
+int mix_expert_combine_grad(const void* y, int dtype, long long ld_y, int y_rows, const float* weights, const int* position, int T, int k, int N,
+                            const void* d_out, long long ld_d, float* d_weights, void* d_y, long long ld_dy, void* stream, char* errbuf,
+                            int errbuf_len);
+
 #ifdef __cplusplus
 }
 #endif

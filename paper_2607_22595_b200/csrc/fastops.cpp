@@ -421,6 +421,36 @@ PyObject* expert_combine(PyObject* const* a) {
   return r.take(0);
 }
 
+// expert_combine_grad(d_out, y, weights, position, want_y, d_weights | None, d_y | None, stream | None)
+PyObject* expert_combine_grad(PyObject* const* a) {
+  const Rows y = rows_of(tensor(a[1], "y", 2), "y");
+  const Tensor& pt = tensor(a[3], "position", ScalarType::Int, 2, &y.t);
+  const int64_t T = pt.size(0), k = pt.size(1);
+  const int* position = dense<int>(pt, "position", {T, k});
+  const float* w = dense<float>(a[2], "weights", ScalarType::Float, {T, k}, y.t);
+  const Rows d = rows_of(tensor(a[0], "d_out", 2, &y.t), "d_out");
+  need(d.n == T && d.m == y.m && d.dtype == y.dtype, "d_out must be [T, N] in y's type");
+  const int want_y = PyObject_IsTrue(a[4]);
+  if (want_y < 0) throw Raised();
+  Call c(y.t.get_device(), a[7]);
+  Results r;
+  float* dw;
+  c.want(a[5], "d_weights", ScalarType::Float, {T, k}, y.t, &dw, &r.o[0]);
+  c.allocate();
+  if (!want_y) {
+    c.run([&](void* s, char* e, int n) {
+      return mix_expert_combine_grad(y.p, y.dtype, y.ld, (int)y.n, w, position, (int)T, (int)k, (int)y.m, d.p, d.ld, dw, nullptr, y.m, s, e, n);
+    });
+    return r.take(0);
+  }
+  const Rows dy = c.result_rows(a[6], "d_y", y.t.scalar_type(), y.n, y.m, y.t, &r.o[1]);
+  need(dy.dtype == y.dtype, "d_y must have y's type");
+  c.run([&](void* s, char* e, int n) {
+    return mix_expert_combine_grad(y.p, y.dtype, y.ld, (int)y.n, w, position, (int)T, (int)k, (int)y.m, d.p, d.ld, dw, dy.p, dy.ld, s, e, n);
+  });
+  return r.tuple(2);
+}
+
 template <PyObject* (*F)(PyObject* const*), int N>
 PyObject* entry(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -447,7 +477,7 @@ PyObject* entry(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define ENTRY(f, n) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(entry<f, n>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(router_topk, 8), ENTRY(router_topk_grad, 8), ENTRY(expert_order, 6), ENTRY(router_balance, 5),
-                         ENTRY(router_balance_grad, 9), ENTRY(quantize_rows, 6), ENTRY(linear_int, 9), ENTRY(expert_combine, 5),
+                         ENTRY(router_balance_grad, 9), ENTRY(quantize_rows, 6), ENTRY(linear_int, 9), ENTRY(expert_combine, 5), ENTRY(expert_combine_grad, 8),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastops", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

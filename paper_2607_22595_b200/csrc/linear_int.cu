@@ -4,6 +4,7 @@
 //   linear_int_kernel      y[t, n] = (sum_i codes[t, i] W[n, i]) scale[t] w_scale[n] + bias[n], the sum exact in 32-bit integers;
 //                         grouped: rows offsets[e] .. offsets[e + 1] go through weight set e
 //   combine_kernel        out[t, :] = sum_j weight[t, j] y[position[t, j], :]
+//   combine_grad_kernel   d_weight[t, j] = <d_out[t, :], y[position[t, j], :]>,  d_y[position[t, j], :] = weight[t, j] d_out[t, :]
 #include "op_common.cuh"
 #include "tc_common.cuh"
 
@@ -607,6 +608,68 @@ combine_kernel(const T* __restrict__ y, long long ld_y, int y_rows, const float*
   }
 }
 
+// The gradients.  A CTA has a token: its d_out is read once for all of the token's rows, and the products are added up in a fixed order
+// (a thread's vectors, the lanes of a warp, the warps).
+constexpr int kCombineGradThreads = 256;
+template <typename T, int KMAX, bool vec>
+__global__ void __launch_bounds__(kCombineGradThreads)
+combine_grad_kernel(const T* __restrict__ y, long long ld_y, int y_rows, const float* __restrict__ weights, const int* __restrict__ position,
+                    int k, int N, const T* __restrict__ d_out, long long ld_d, float* __restrict__ d_weights, T* __restrict__ d_y,
+                    long long ld_dy) {
+  constexpr int VW = vec ? RowVec<T>::VW : 1;
+  __shared__ float part[kCombineGradThreads / 32][KMAX];
+  pdl_wait();
+  pdl_launch_dependents();
+  const long long t = blockIdx.x;
+  int at[KMAX];
+  float w[KMAX], dot[KMAX];
+#pragma unroll
+  for (int j = 0; j < KMAX; ++j) {
+    at[j] = j < k ? position[t * k + j] : -1;
+    w[j] = j < k && d_y ? weights[t * k + j] : 0.f;
+    dot[j] = 0.f;
+  }
+  for (long long c = (long long)threadIdx.x * VW; c < N; c += kCombineGradThreads * VW) {
+    const int n = (int)min((long long)VW, N - c);              // (fewer than a vector at the row's end)
+    __align__(16) T g[VW];
+    if (vec && n == VW) *reinterpret_cast<uint4*>(g) = *reinterpret_cast<const uint4*>(d_out + t * ld_d + c);
+    else
+      for (int i = 0; i < VW; ++i) g[i] = i < n ? d_out[t * ld_d + c + i] : from_f32<T>(0.f);
+#pragma unroll
+    for (int j = 0; j < KMAX; ++j) {
+      if ((unsigned)at[j] >= (unsigned)y_rows) continue;
+      const T* row = y + at[j] * ld_y + c;
+      __align__(16) T e[VW], d[VW];
+      if (vec && n == VW) *reinterpret_cast<uint4*>(e) = *reinterpret_cast<const uint4*>(row);
+      else
+        for (int i = 0; i < VW; ++i) e[i] = i < n ? row[i] : from_f32<T>(0.f);
+#pragma unroll
+      for (int i = 0; i < VW; ++i) {
+        dot[j] = fmaf(to_f32(g[i]), to_f32(e[i]), dot[j]);
+        d[i] = from_f32<T>(w[j] * to_f32(g[i]));
+      }
+      if (d_y) {
+        T* to = d_y + at[j] * ld_dy + c;
+        if (vec && n == VW) *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(d);
+        else
+          for (int i = 0; i < n; ++i) to[i] = d[i];
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < KMAX; ++j) {
+    const float s = group_sum<32>(dot[j]);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5][j] = s;
+  }
+  __syncthreads();
+  if (threadIdx.x < k) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < kCombineGradThreads / 32; ++i) s += part[i][threadIdx.x];
+    d_weights[t * k + threadIdx.x] = s;
+  }
+}
+
 // ---------------------------------------------------------------------------------------------------- host side
 struct Gemm {
   const void* codes;
@@ -786,6 +849,26 @@ cudaError_t combine_launch(const void* y, long long ld_y, int y_rows, const floa
              : combine_launch_as<T, false>(y, ld_y, y_rows, weights, position, T_rows, k, N, out, ld_out, s);
 }
 
+template <typename T, bool vec>
+cudaError_t combine_grad_launch_as(const void* y, long long ld_y, int y_rows, const float* weights, const int* position, int T_rows, int k, int N,
+                                   const void* d_out, long long ld_d, float* d_weights, void* d_y, long long ld_dy, cudaStream_t s) {
+#define MIX_COMBINE_GRAD(K)                                                                                                                   \
+  return launch_pdl(kPdlHook, combine_grad_kernel<T, K, vec>, dim3((unsigned)T_rows), dim3(kCombineGradThreads), 0, s, static_cast<const T*>(y), ld_y, \
+                    y_rows, weights, position, k, N, static_cast<const T*>(d_out), ld_d, d_weights, static_cast<T*>(d_y), ld_dy)
+  if (k <= 2) MIX_COMBINE_GRAD(2);
+  if (k <= 8) MIX_COMBINE_GRAD(8);
+  MIX_COMBINE_GRAD(kOpMaxTopk);
+#undef MIX_COMBINE_GRAD
+}
+template <typename T>
+cudaError_t combine_grad_launch(const void* y, long long ld_y, int y_rows, const float* weights, const int* position, int T_rows, int k, int N,
+                                const void* d_out, long long ld_d, float* d_weights, void* d_y, long long ld_dy, cudaStream_t s) {
+  const long long es = sizeof(T);
+  const bool vec = (((uintptr_t)y | (uintptr_t)d_out | (uintptr_t)d_y | (uintptr_t)(ld_y * es) | (uintptr_t)(ld_d * es) | (uintptr_t)(d_y ? ld_dy * es : 0)) & 15u) == 0;
+  return vec ? combine_grad_launch_as<T, true>(y, ld_y, y_rows, weights, position, T_rows, k, N, d_out, ld_d, d_weights, d_y, ld_dy, s)
+             : combine_grad_launch_as<T, false>(y, ld_y, y_rows, weights, position, T_rows, k, N, d_out, ld_d, d_weights, d_y, ld_dy, s);
+}
+
 }  // namespace
 
 extern "C" int mix_quantize_rows(const void* x, int dtype, long long ld, int x_rows, const int* order, int k, int n_rows, int d,
@@ -841,5 +924,24 @@ extern "C" int mix_expert_combine(const void* y, int dtype, long long ld_y, int 
   if (dtype == MIX_DTYPE_F32) MIX_OP_CUDA(combine_launch<float>(y, ld_y, y_rows, weights, position, T, k, N, out, ld_out, s));
   else if (dtype == MIX_DTYPE_BF16) MIX_OP_CUDA(combine_launch<__nv_bfloat16>(y, ld_y, y_rows, weights, position, T, k, N, out, ld_out, s));
   else MIX_OP_CUDA(combine_launch<__half>(y, ld_y, y_rows, weights, position, T, k, N, out, ld_out, s));
+  return MIX_OK;
+}
+
+extern "C" int mix_expert_combine_grad(const void* y, int dtype, long long ld_y, int y_rows, const float* weights, const int* position, int T, int k,
+                                       int N, const void* d_out, long long ld_d, float* d_weights, void* d_y, long long ld_dy, void* stream,
+                                       char* errbuf, int errbuf_len) {
+  if (op_elem_size(dtype) == 0) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "dtype %d is no MIX_DTYPE_*", dtype);
+  if (T < 0 || y_rows < 0 || T > kOpMaxRows) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "%d tokens, %d rows of y", T, y_rows);
+  if (k < 1 || k > kOpMaxTopk) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "k %d outside [1, %d]", k, kOpMaxTopk);
+  if (N < 1 || N > MIX_COMBINE_MAX_N) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "N %d outside [1, %d]", N, MIX_COMBINE_MAX_N);
+  if (ld_y < N || ld_d < N || (d_y && ld_dy < N)) MIX_OP_FAIL(MIX_ERR_OUT_OF_RANGE, "row strides %lld, %lld, %lld below N %d", ld_y, ld_d, ld_dy, N);
+  if (T == 0) return MIX_OK;
+  if ((!y && y_rows > 0) || !position || !d_out || !d_weights || (d_y && !weights))
+    MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "y, position, d_out, d_weights (and weights for d_y) are required");
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (dtype == MIX_DTYPE_F32) MIX_OP_CUDA(combine_grad_launch<float>(y, ld_y, y_rows, weights, position, T, k, N, d_out, ld_d, d_weights, d_y, ld_dy, s));
+  else if (dtype == MIX_DTYPE_BF16)
+    MIX_OP_CUDA(combine_grad_launch<__nv_bfloat16>(y, ld_y, y_rows, weights, position, T, k, N, d_out, ld_d, d_weights, d_y, ld_dy, s));
+  else MIX_OP_CUDA(combine_grad_launch<__half>(y, ld_y, y_rows, weights, position, T, k, N, d_out, ld_d, d_weights, d_y, ld_dy, s));
   return MIX_OK;
 }

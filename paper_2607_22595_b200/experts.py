@@ -93,3 +93,9 @@ def linear_int_status(stream=None) -> int:
 def expert_combine(y, weights, position, out=None, stream=None):
     """out[t] = sum_j weights[t, j] y[position[t, j]] -> [T, N] in y's type.  y [n, N] in expert_order's order; entries of -1 do not count."""
     return (B._ops or _ops()).expert_combine(y, weights, position, out, stream)
+
+
+def expert_combine_grad(d_out, y, weights, position, want_y=False, d_weights=None, d_y=None, stream=None):
+    """Gradients of expert_combine for d_out [T, N]: d_weights fp32 [T, k] -- router_topk_grad takes it from there -- and with want_y
+    also d_y [n, N], of which rows that no entry of `position` names are left as they were (uninitialised if d_y is not given)."""
+    return (B._ops or _ops()).expert_combine_grad(d_out, y, weights, position, want_y, d_weights, d_y, stream)

@@ -431,3 +431,97 @@ def test_refused_tensors():
                  lambda: mix.linear_int(codes[:, :40].contiguous(), scale, W[:, :40].contiguous(), w_scale)):
         with pytest.raises(mix.MixError):
             call()
+
+
+@pytest.mark.parametrize("T,k,N,dtype", [(1, 1, 1, "bf16"), (5, 2, 8, "fp32"), (7, 3, 100, "fp16"), (40, 8, 4096, "bf16"), (3, 16, 5000, "fp32"), (9, 2, 8200, "bf16"),
+                                         (700, 6, 64, "bf16"), (0, 2, 16, "fp32")])
+@pytest.mark.parametrize("pad", [0, 1, 8])
+def test_gradients_of_combine(T, k, N, dtype, pad):
+    g = torch.Generator(device=DEV).manual_seed(T + N)
+    n = T * k + 3
+    y = torch.randn((n, N + pad), generator=g, device=DEV).to(DTYPES[dtype])[:, :N]
+    d_out = torch.randn((T, N + pad), generator=g, device=DEV).to(DTYPES[dtype])[:, :N]
+    w = torch.randn((T, k), generator=g, device=DEV)
+    position = torch.randperm(n, generator=g, device=DEV)[:T * k].int().view(T, k)
+    if T > 4:
+        position[0] = -1
+        position[1, 0] = n
+        w[0] = torch.nan
+    d_y = torch.full((n, N + pad), 6.0, dtype=y.dtype, device=DEV)
+    d_w, got = mix.expert_combine_grad(d_out, y, w, position, want_y=True, d_y=d_y[:, :N])
+    assert torch.equal(mix.expert_combine_grad(d_out, y, w, position), d_w)
+    there = (position >= 0) & (position < n)
+    at = position.clamp(0, n - 1).long()
+    terms = torch.where(there[:, :, None], d_out.double()[:, None] * y[at].double(), 0.0)
+    # a thread's share one after the other (N / 256 additions, vectors of 8 within), a tree of 8 steps over the block
+    R.within(d_w, terms.sum(2), (N / 256 + 8 + 16) * R.U * terms.abs().sum(2) + 1e-37, "d_weights")
+    want = torch.full((n, N), 6.0, dtype=torch.float64, device=DEV)
+    want[at[there]] = (w[:, :, None].double() * d_out.double()[:, None])[there]
+    R.within(d_y[:, :N], want, R.U * want.abs() + R.rounding(y.dtype, want), "d_y")
+    assert (d_y[:, N:] == 6).all() and torch.equal(got, d_y[:, :N])
+
+
+def test_the_gradient_of_a_steering_against_differences():
+    """A loss on the layer's output and its balance, through the sum over experts, the selection and the steering: all in one step, captured
+    and replayed, against differences of the same in 64 bits (the chosen experts and their results held)."""
+    T, E, k, K, N = 48, 12, 3, 64, 40
+    g = torch.Generator(device=DEV).manual_seed(3)
+    base = 1.5 * torch.randn((T, E), generator=g, device=DEV)
+    delta = 0.3 * torch.randn(E, generator=g, device=DEV)
+    hidden = torch.randn((T, K), generator=g, device=DEV).to(torch.bfloat16)
+    W, w_scale = mix.quantize_rows((torch.randn((E * N, K), generator=g, device=DEV) / 8).to(torch.bfloat16))
+    W, w_scale = W.view(E, N, K), w_scale.view(E, N)
+    d_out = torch.randn((T, N), generator=g, device=DEV)
+    seg = torch.tensor([0, 20, T], dtype=torch.int32, device=DEV)
+    d_loss = torch.tensor([0.7, -0.4], device=DEV)
+    m = mix.Mix(d_model=64, T_max=T, n_slots_max=1)
+    m.register_router(0, delta)
+    m.set_slot_map(torch.zeros(T, dtype=torch.int32, device=DEV))
+    logits = torch.empty_like(base)
+
+    def step():
+        logits.copy_(base)
+        m.apply_router(logits)
+        idx, w = mix.router_topk(logits, k)
+        offsets, order, position = mix.expert_order(idx, E)
+        codes, scale = mix.quantize_rows(hidden, order=order, k=k)
+        y = mix.linear_int_grouped(codes, scale, W, w_scale, offsets, dtype=torch.float32)
+        d_w = mix.expert_combine_grad(d_out, y, w, position)
+        loss, counts, _, rows = mix.router_balance(logits, idx, seg)
+        d = mix.router_topk_grad(logits, idx, w, d_w)
+        b = mix.router_balance_grad(logits, idx, counts, rows, d_loss, seg)
+        return idx, position, y, d, b
+
+    eager = [t.clone() for t in step()]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    graph.replay()
+    assert all(torch.equal(a, b) for a, b in zip(eager, out))
+    idx, position, y, d, b = (t.cpu() for t in eager)
+    y64, i64, p = y.double(), idx.long(), position.long()
+    base64, G, seg64 = base.cpu().double(), d_out.cpu().double(), seg.tolist()
+    dl = d_loss.cpu().double()
+
+    def f(x):
+        w = R.weights_of(x, i64, "softmax", True)
+        return ((w[:, :, None] * y64[p]).sum(1) * G).sum() + (R.balance(x, i64, seg64, "softmax")[0] * dl).sum()
+
+    # base + delta is rounded to fp32 by the steering: the differences are taken around what it gave
+    x = (base.cpu() + delta.cpu()).double()
+    assert torch.equal(logits.cpu().double(), x)
+    d_delta = (d.double() + b.double()).sum(0)
+    # the kernel's own error: of the weights' gradients (their dot products and the selection's bound), of the balance's
+    d_w = (G[:, None] * y64[p]).sum(2)
+    size_w = (G[:, None] * y64[p]).abs().sum(2)
+    _, size = R.topk_grad(x, i64, "softmax", True, size_w)
+    _, bsize = R.balance_grad(x, i64, seg64, "softmax", dl)
+    own = ((2 * R.rel_p(x, "softmax") + 60 * R.U) * (size + bsize)).sum(0)
+    h = 1e-5
+    for e in range(E):
+        up = x.clone(); up[:, e] += h
+        down = x.clone(); down[:, e] -= h
+        change = (f(up) - f(down)) / (2 * h)
+        # of the differences: 2^-53 |f| / h and h^2 / 6 times third derivatives of at most 6 sum |d_w| (and 6 E)
+        assert abs(change - d_delta[e]) <= own[e] + 1e-10 * (6 * d_w.abs().sum() + 6 * E) + 1e-9, e
+    m.destroy()

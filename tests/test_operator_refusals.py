@@ -12,10 +12,10 @@ SMALL_NORMAL = dict(topk=[P, 0, 8, 4, 8, 2, 1, 1, None, P, P], topk_grad=[P, 0, 
                     order=[P, 8, 8, P, P, P, None, 0], balance=[P, 0, 8, P, 4, 8, 2, 1, None, 1, P, P, P, P, P, 1 << 20],
                     balance_grad=[P, 0, 8, P, 4, 8, 2, 1, None, 1, P, P, P, P, 8], quantize=[P, 1, 64, 4, None, 1, 4, 64, P, P],
                     linear=[P, P, 4, 64, P, P, 8, None, P, 1, 8], grouped=[P, P, 4, 64, P, P, 2, 8, P, None, P, 1, 8],
-                    combine=[P, 1, 8, 8, P, P, 4, 2, 8, P, 8])
+                    combine=[P, 1, 8, 8, P, P, 4, 2, 8, P, 8], combine_grad=[P, 1, 8, 8, P, P, 4, 2, 8, P, 8, P, P, 8])
 FN = dict(topk="mix_router_topk", topk_grad="mix_router_topk_grad", order="mix_expert_order", balance="mix_router_balance",
           balance_grad="mix_router_balance_grad", quantize="mix_quantize_rows", linear="mix_linear_int", grouped="mix_linear_int_grouped",
-          combine="mix_expert_combine")
+          combine="mix_expert_combine", combine_grad="mix_expert_combine_grad")
 REFUSED = [
     ("topk", {0: None}, INVALID), ("topk", {1: 3}, INVALID), ("topk", {2: 7}, RANGE), ("topk", {3: -1}, RANGE), ("topk", {3: (1 << 30) + 1}, RANGE), ("balance", {4: (1 << 30) + 1}, RANGE),
     ("linear", {2: (1 << 30) + 1}, RANGE), ("linear", {2: 1 << 30, 6: 1 << 20, 10: 1 << 20}, RANGE), ("quantize", {6: (1 << 30) + 1, 3: (1 << 30) + 1}, RANGE),
@@ -37,6 +37,9 @@ REFUSED = [
     ("grouped", {8: None}, INVALID), ("grouped", {6: 0}, RANGE), ("grouped", {6: 513}, RANGE), ("grouped", {6: 512, 7: 1 << 23, 12: 1 << 23}, RANGE),
     ("combine", {0: None}, INVALID), ("combine", {1: 9}, INVALID), ("combine", {2: 7}, RANGE), ("combine", {7: 0}, RANGE), ("combine", {7: 17}, RANGE),
     ("combine", {8: 0}, RANGE), ("combine", {8: 8388481, 2: 8388481, 10: 8388481}, RANGE), ("combine", {10: 7}, RANGE), ("combine", {5: None}, INVALID),
+    ("combine_grad", {1: 3}, INVALID), ("combine_grad", {6: -1}, RANGE), ("combine_grad", {7: 17}, RANGE), ("combine_grad", {8: 0}, RANGE),
+    ("combine_grad", {2: 7}, RANGE), ("combine_grad", {10: 7}, RANGE), ("combine_grad", {13: 7}, RANGE), ("combine_grad", {4: None}, INVALID),
+    ("combine_grad", {9: None}, INVALID), ("combine_grad", {11: None}, INVALID),
 ]
 
 
@@ -67,6 +70,6 @@ def test_tensors_of_the_host_are_refused():
     for call in (lambda: mix.router_topk(x, 2), lambda: mix.router_topk_grad(x, i, x, x), lambda: mix.expert_order(i, 8), lambda: mix.router_balance(x, i),
                  lambda: mix.router_balance_grad(x, i, i, i, x), lambda: mix.quantize_rows(x.bfloat16()),
                  lambda: mix.linear_int(x.char(), x, x.char(), x), lambda: mix.linear_int_grouped(x.char(), x, x.char(), x, i),
-                 lambda: mix.expert_combine(x, x, i)):
+                 lambda: mix.expert_combine(x, x, i), lambda: mix.expert_combine_grad(x, x, x, i)):
         with pytest.raises(ValueError):
             call()
