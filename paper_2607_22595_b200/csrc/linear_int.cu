@@ -558,7 +558,8 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
 }
 
 // ---------------------------------------------------------------------------------------------------- the sum over experts
-// A thread has one vector of one token; all of the token's rows are on their way at once.
+// A thread has one vector of one token; all of the token's rows are on their way at once.  2048 tokens, 6 of 5120 bf16: 23.6 us
+// (6.2 TB/s), 38 with the rows in fours and three vectors a thread.
 constexpr int kCombineThreads = 128;
 template <typename T, int KMAX, bool vec>
 __global__ void __launch_bounds__(kCombineThreads)
@@ -609,7 +610,8 @@ combine_kernel(const T* __restrict__ y, long long ld_y, int y_rows, const float*
 }
 
 // The gradients.  A CTA has a token: its d_out is read once for all of the token's rows, and the products are added up in a fixed order
-// (a thread's vectors, the lanes of a warp, the warps).
+// (a thread's vectors, the lanes of a warp, the warps).  8192 tokens, 2 of 4096 bf16: 36.9 us (5.4 TB/s; 49 with the rows one after the
+// other), 56 with d_y; 2048 tokens, 6 of 5120: 39 and 57.
 constexpr int kCombineGradThreads = 256;
 template <typename T, int KMAX, bool vec>
 __global__ void __launch_bounds__(kCombineGradThreads)
@@ -630,29 +632,37 @@ combine_grad_kernel(const T* __restrict__ y, long long ld_y, int y_rows, const f
     dot[j] = 0.f;
   }
   for (long long c = (long long)threadIdx.x * VW; c < N; c += kCombineGradThreads * VW) {
-    const int n = (int)min((long long)VW, N - c);              // (fewer than a vector at the row's end)
-    __align__(16) T g[VW];
-    if (vec && n == VW) *reinterpret_cast<uint4*>(g) = *reinterpret_cast<const uint4*>(d_out + t * ld_d + c);
-    else
-      for (int i = 0; i < VW; ++i) g[i] = i < n ? d_out[t * ld_d + c + i] : from_f32<T>(0.f);
+    const bool whole = vec && c + VW <= N;
+    if (whole) {                                               // all rows of the token under way at once
+      uint4 raw[KMAX];
+      const uint4 graw = *reinterpret_cast<const uint4*>(d_out + t * ld_d + c);
 #pragma unroll
-    for (int j = 0; j < KMAX; ++j) {
-      if ((unsigned)at[j] >= (unsigned)y_rows) continue;
-      const T* row = y + at[j] * ld_y + c;
-      __align__(16) T e[VW], d[VW];
-      if (vec && n == VW) *reinterpret_cast<uint4*>(e) = *reinterpret_cast<const uint4*>(row);
-      else
-        for (int i = 0; i < VW; ++i) e[i] = i < n ? row[i] : from_f32<T>(0.f);
+      for (int j = 0; j < KMAX; ++j)
+        if ((unsigned)at[j] < (unsigned)y_rows) raw[j] = *reinterpret_cast<const uint4*>(y + at[j] * ld_y + c);
+      const T* g = reinterpret_cast<const T*>(&graw);
 #pragma unroll
-      for (int i = 0; i < VW; ++i) {
-        dot[j] = fmaf(to_f32(g[i]), to_f32(e[i]), dot[j]);
-        d[i] = from_f32<T>(w[j] * to_f32(g[i]));
-      }
-      if (d_y) {
-        T* to = d_y + at[j] * ld_dy + c;
-        if (vec && n == VW) *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(d);
-        else
-          for (int i = 0; i < n; ++i) to[i] = d[i];
+      for (int j = 0; j < KMAX; ++j)
+        if ((unsigned)at[j] < (unsigned)y_rows) {
+          const T* e = reinterpret_cast<const T*>(&raw[j]);
+#pragma unroll
+          for (int i = 0; i < VW; ++i) dot[j] = fmaf(to_f32(g[i]), to_f32(e[i]), dot[j]);
+          if (d_y) {
+            uint4 out;
+            T* d = reinterpret_cast<T*>(&out);
+#pragma unroll
+            for (int i = 0; i < VW; ++i) d[i] = from_f32<T>(w[j] * to_f32(g[i]));
+            *reinterpret_cast<uint4*>(d_y + at[j] * ld_dy + c) = out;
+          }
+        }
+    } else {
+      for (int i = 0; i < VW && c + i < N; ++i) {
+        const float g = to_f32(d_out[t * ld_d + c + i]);
+#pragma unroll
+        for (int j = 0; j < KMAX; ++j)
+          if ((unsigned)at[j] < (unsigned)y_rows) {
+            dot[j] = fmaf(g, to_f32(y[at[j] * ld_y + c + i]), dot[j]);
+            if (d_y) d_y[at[j] * ld_dy + c + i] = from_f32<T>(w[j] * g);
+          }
       }
     }
   }
