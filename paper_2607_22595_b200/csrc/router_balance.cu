@@ -189,7 +189,8 @@ balance_kernel(const T* __restrict__ logits, long long ld, int vec, const int* _
 
 // One segment per cluster: CTA r of the cluster adds up the r-th part of the segment's slots, CTA 0 puts the parts together.
 // Sums in 64 bits: there are few, and a long request has thousands of slots.
-template <int cluster>
+// (as many threads as experts where requests are short: there are many such CTAs)
+template <int cluster, bool kShort>
 __global__ void __launch_bounds__(kFinThreads)
 balance_finish_kernel(const float* __restrict__ part_p, const int* __restrict__ part_c, const int* __restrict__ part_n, int T_rows, int E,
                       const int* __restrict__ seg, int unit_rows, float* __restrict__ loss, int* __restrict__ counts,
@@ -204,6 +205,7 @@ balance_finish_kernel(const float* __restrict__ part_p, const int* __restrict__ 
   pdl_wait();
   pdl_launch_dependents();
   const int s = blockIdx.x / cluster, rank = blockIdx.x % cluster, tid = threadIdx.x;
+  const int threads = kShort ? (int)blockDim.x : kFinThreads;
   const int a = seg_at(seg, s, T_rows), b = seg_at(seg, s + 1, T_rows);
   int u0 = 0, u1 = 0;                                          // units that the segment touches
   if (a < b) {
@@ -216,11 +218,11 @@ balance_finish_kernel(const float* __restrict__ part_p, const int* __restrict__ 
   __syncthreads();
   {
     int n = 0;
-    for (int u = v0 + tid; u < v1; u += kFinThreads) n += part_n[u + s];
+    for (int u = v0 + tid; u < v1; u += threads) n += part_n[u + s];
     n = __reduce_add_sync(0xffffffffu, n);
     if ((tid & 31) == 0 && n) atomicAdd(&sn, n);
   }
-  const int wide = min((E + 31) & ~31, kFinThreads), lanes = kFinThreads / wide;    // E <= 512 = kFinThreads: one pass
+  const int wide = (E + 31) & ~31, lanes = threads / wide;     // (threads >= wide: one pass)
   const int e = tid % wide, part = tid / wide;
   double p = 0.0;
   int c = 0;
@@ -287,7 +289,7 @@ balance_finish_kernel(const float* __restrict__ part_p, const int* __restrict__ 
     }
     __syncthreads();
     if (tid == 0) {
-      for (int w = 1; w < kFinThreads / 32; ++w) {
+      for (int w = 1; w < threads / 32; ++w) {
         fp += red[w];
         total += red_c[w];
       }
@@ -394,8 +396,10 @@ struct Plan {
   long long slots;
 };
 // Small calls (up to 16384 logits): a CTA per segment, one launch, which even one segment of all rows finishes in a few trips.
-// Otherwise units of eight warps where the average request has 64 rows or more: one wave of CTAs, of at least 64 rows.  Where
-// requests are short (decode steps: one row each) a unit is one warp with 32 rows, and no barrier stands between two requests.
+// Otherwise units of eight warps where the average request has 64 rows or more: one wave of CTAs, of at least 32 rows (64 requests in
+// 8192 rows of 64 bf16: 9.8 us, 11.3 with 64 rows).  Where requests are short (decode steps: one row each) a unit is one warp and no
+// barrier stands between two requests; each costs it a microsecond and a half, so a unit has 4 rows as long as the SMs hold all
+// units at once (1024 requests of one row, 64 experts: 10.6 us, 46 with 32 rows).
 constexpr int kDirectLogits = 16384;
 Plan plan(int T, int E, int n_seg, int n_sms) {
   Plan p;
@@ -403,9 +407,9 @@ Plan plan(int T, int E, int n_seg, int n_sms) {
   p.warps = T / n_seg >= 64 ? kUnitWarps : 1;
   if (p.warps == kUnitWarps) {
     p.unit_rows = (T + kUnitCtas * n_sms - 1) / (kUnitCtas * n_sms);
-    if (p.unit_rows < 64) p.unit_rows = 64;
+    if (p.unit_rows < 32) p.unit_rows = 32;
   } else {
-    p.unit_rows = 32;
+    p.unit_rows = T <= 8 * 32 * n_sms ? 4 : 32;
   }
   p.units = T > 0 ? (T + p.unit_rows - 1) / p.unit_rows : 0;
   p.slots = p.direct ? 0 : (long long)p.units + n_seg;
@@ -499,7 +503,7 @@ extern "C" int mix_router_balance(const void* logits, int dtype, long long ld, c
   if (p.direct) return MIX_OK;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(n_seg * p.cluster));
-  cfg.blockDim = dim3(kFinThreads);
+  cfg.blockDim = dim3(p.warps == 1 && p.cluster == 1 ? ((n_experts + 31) & ~31) : kFinThreads);
   cfg.stream = s;
   cudaLaunchAttribute at[2];
   int n_at = 0;
@@ -515,7 +519,7 @@ extern "C" int mix_router_balance(const void* logits, int dtype, long long ld, c
   }
   cfg.attrs = at;
   cfg.numAttrs = n_at;
-  MIX_OP_CUDA(cudaLaunchKernelEx(&cfg, p.cluster > 1 ? balance_finish_kernel<kFinCluster> : balance_finish_kernel<1>, static_cast<const float*>(part_p),
+  MIX_OP_CUDA(cudaLaunchKernelEx(&cfg, p.cluster > 1 ? balance_finish_kernel<kFinCluster, false> : (p.warps == 1 ? balance_finish_kernel<1, true> : balance_finish_kernel<1, false>), static_cast<const float*>(part_p),
                                  static_cast<const int*>(part_c), static_cast<const int*>(part_n), T, n_experts, seg, p.unit_rows, loss, counts,
                                  mean_p, rows));
   return MIX_OK;
