@@ -22,7 +22,9 @@ using namespace mix;
 namespace {
 
 constexpr int kUnitWarps = 8;              // warps of a unit where requests are long
-constexpr int kUnitCtas = 4, kGradCtas = 4; // CTAs an SM holds at a time: large batches make one wave of them
+// CTAs an SM holds at a time: large batches make one wave of them.  Above 256 experts, with 16 logits a lane, that spills 140 bytes and is
+// faster all the same: 32768 rows of 512 fp32, forward 23.7 us and backward 31.3, 27.1 and 32.7 with three and two CTAs.
+constexpr int kUnitCtas = 4, kGradCtas = 4;
 constexpr int kFinThreads = 512;
 constexpr int kFinCluster = 8;
 
