@@ -150,12 +150,15 @@ __device__ __forceinline__ float exp2_hw(float x) {
 constexpr float kLog2e = 1.44269502162933350f;
 __device__ __forceinline__ float exp_row(float x) { return exp2_hw(x * kLog2e); }
 // e^(x - top), with top log2 e at hand: one multiply-add, which rounds once.  What the rounding of top log2 e is off is a factor that
-// all logits of the row have in common.  (Sizes above 10^38, where it would leave fp32's range, are subtracted first.)
+// all logits of the row have in common: within 2^(+-2^-8) up to |top| = 65536, whose product with log2 e is below 2^17.  Beyond, the
+// factor would grow, and leave fp32's range from 1.4e9 on, so there the difference is taken first.  It is exact for every logit
+// that has a score other than 0, one within 104 of such a top.
+constexpr float kFarTop = 65536.f;
 struct ExpFrom {
   float top, scaled;
-  bool large;
-  __device__ __forceinline__ explicit ExpFrom(float t) : top(t), scaled(t * kLog2e), large(fabsf(t) > 1e38f) {}
-  __device__ __forceinline__ float operator()(float x) const { return large ? exp_row(x - top) : exp2_hw(fmaf(x, kLog2e, -scaled)); }
+  bool far;
+  __device__ __forceinline__ explicit ExpFrom(float t) : top(t), scaled(t * kLog2e), far(fabsf(t) > kFarTop) {}
+  __device__ __forceinline__ float operator()(float x) const { return far ? exp_row(x - top) : exp2_hw(fmaf(x, kLog2e, -scaled)); }
 };
 __device__ __forceinline__ float rcp_hw(float x) {
   float y;
