@@ -19,6 +19,7 @@
 #include <climits>
 #include <cstdarg>
 #include <initializer_list>
+#include <optional>
 #include <stdexcept>
 #include <string>
 
@@ -106,19 +107,23 @@ long long integer(PyObject* o, const char* name, long long lo, long long hi) {
 }
 
 // One call: its device made current, its stream, and what it allocates, in order.
+// A stream that is given is made current as well, so that outputs and scratch memory are the given stream's: what the allocator gave back
+// on the stream that was current may still be used by work queued there.  The outputs are then marked as used by that one, on which
+// the caller is likely to read and to drop them.
 struct Call {
   c10::cuda::OptionalCUDAGuard guard;
+  c10::cuda::OptionalCUDAStreamGuard as_current;
   int device;
   cudaStream_t stream;
-  bool elsewhere = false;                        // not the device's current stream: memory it uses is marked so
-  Tensor made[8];
+  std::optional<c10::cuda::CUDAStream> before;   // the current stream, where another one is given
+  Tensor made[8], scratch_memory;
   int n_made = 0;
 
   Call(int dev, PyObject* s) : device(dev) {
     if (c10::cuda::current_device() != dev) guard.set_index(dev);
-    const cudaStream_t now = c10::cuda::getCurrentCUDAStream(dev).stream();
+    const c10::cuda::CUDAStream now = c10::cuda::getCurrentCUDAStream(dev);
     if (s == Py_None) {
-      stream = now;
+      stream = now.stream();
       return;
     }
     PyObject* v = PyObject_GetAttrString(s, "cuda_stream");
@@ -130,11 +135,17 @@ struct Call {
     stream = static_cast<cudaStream_t>(PyLong_AsVoidPtr(v));
     Py_DECREF(v);
     if (!stream && PyErr_Occurred()) throw Raised();
-    elsewhere = stream != now;
+    if (stream == now.stream()) return;
+    before = now;
+    as_current.reset_stream(stream ? c10::cuda::getStreamFromExternal(stream, (c10::DeviceIndex)dev)
+                                   : c10::cuda::getDefaultCUDAStream((c10::DeviceIndex)dev));
+  }
+  Tensor allocated(at::IntArrayRef shape, ScalarType type) const {
+    return Tensor(at::detail::empty_cuda(shape, type, c10::Device(c10::kCUDA, (c10::DeviceIndex)device), std::nullopt));
   }
   Tensor& empty(at::IntArrayRef shape, ScalarType type) {
     Tensor& t = made[n_made++];
-    t = Tensor(at::detail::empty_cuda(shape, type, c10::Device(c10::kCUDA, (c10::DeviceIndex)device), std::nullopt));
+    t = allocated(shape, type);
     return t;
   }
   // The dense outputs of the call, in the order of the returned tuple: given (checked), or new.  New ones are pieces of one
@@ -193,7 +204,9 @@ struct Call {
   }
   void* scratch(long long bytes) {
     if (bytes < 0) throw Failed{(int)bytes, "the sizes are out of range"};
-    return bytes == 0 ? nullptr : empty({(int64_t)bytes}, ScalarType::Byte).data_ptr();
+    if (bytes == 0) return nullptr;
+    scratch_memory = allocated({(int64_t)bytes}, ScalarType::Byte);
+    return scratch_memory.data_ptr();
   }
   template <typename F>
   void run(F f) {
@@ -202,12 +215,9 @@ struct Call {
     Py_BEGIN_ALLOW_THREADS
     rc = f(static_cast<void*>(stream), text, (int)sizeof text);
     Py_END_ALLOW_THREADS
-    if (elsewhere)
+    if (before)
       for (int i = 0; i < n_made; ++i)
-        if (made[i].numel() > 0)
-          c10::cuda::CUDACachingAllocator::recordStream(made[i].storage().data_ptr(),
-                                                        stream ? c10::cuda::getStreamFromExternal(stream, (c10::DeviceIndex)device)
-                                                               : c10::cuda::getDefaultCUDAStream((c10::DeviceIndex)device));
+        if (made[i].numel() > 0) c10::cuda::CUDACachingAllocator::recordStream(made[i].storage().data_ptr(), *before);
     if (rc != MIX_OK) throw Failed{rc, text};
   }
 };

@@ -8,9 +8,10 @@
     out = mix.expert_combine(y, weights, position)                  # summed over each token's experts
     loss, counts, mean_p, rows = mix.router_balance(logits, idx, seg)   # what the steering did to each request's load
 
-Every function works on the device of its tensors, on the stream given or that device's current one.  Outputs that are not given
-are allocated by torch on that device's current stream (those of one call share one allocation); with a stream of your own, that stream must come behind whatever the memory
-was used for before, as it does when it is the current one.  Gradients are functions of their own: nothing here records a graph.
+Every function works on the device of its tensors, on the stream given or that device's current one.  Outputs that are not given, and
+scratch memory, are allocated by torch on that stream (outputs of one call share one allocation); inputs and outputs that are given must be
+ready there, and whoever reads the results on another stream waits for that one first.  Gradients
+are functions of their own: nothing here records a graph.
 A tensor of the wrong type, shape or place raises ValueError, what the library refuses MixError.
 The C ABI (include/mix.h) states the arithmetic; the checks and the calls into it are in csrc/fastops.cpp.
 """
