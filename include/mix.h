@@ -605,6 +605,11 @@ int mix_linear_int_grouped(const signed char* codes, const float* scale, int n_r
    inside a product kernel ran out, in which case the results since the last call are invalid.  Synchronises `stream`; not capturable. */
 int mix_linear_int_status(unsigned* bits, void* stream, char* errbuf, int errbuf_len);
 
+/* Test hook for the time-out path, as MIX_FLAG_TEST_STALL_ENCODE is: products launched while `on` != 0 (of the whole process) never
+   receive their operands and every bounded wait is capped at ~1 ms, so each CTA gives up, raises MIX_STATUS_WAIT_TIMEOUT, frees its tensor
+   memory and returns; `out` is not meaningful.  Returns the previous setting. */
+int mix_debug_linear_int_stall(int on);
+
 /* The experts' results summed over each token's experts: out[t, :] = sum_j weights[t, j] y[position[t, j], :], j rising, in fp32, rounded
    once.  y: dtype [y_rows, N], rows ld_y apart, in mix_expert_order()'s order; position int32 [T, k] from the same call, entries outside
    [0, y_rows) do not count (nor what stands in their weights).  out: dtype [T, N], rows ld_out apart; a token without experts gets zeros.

@@ -38,7 +38,7 @@ EXPORTS = [
     "mix_bench_param_update", "mix_set_pdl_mask", "mix_debug_phase_clocks",
     "mix_router_topk", "mix_router_topk_grad", "mix_expert_order", "mix_expert_order_workspace", "mix_router_balance",
     "mix_router_balance_workspace", "mix_router_balance_grad", "mix_quantize_rows", "mix_linear_int", "mix_linear_int_grouped",
-    "mix_linear_int_status", "mix_expert_combine", "mix_expert_combine_grad",
+    "mix_linear_int_status", "mix_debug_linear_int_stall", "mix_expert_combine", "mix_expert_combine_grad",
 ]
 
 
@@ -131,6 +131,7 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.mix_linear_int.argtypes = [vp, vp, ci, ci, vp, vp, ci, vp, vp, ci, ll] + err
     lib.mix_linear_int_grouped.argtypes = [vp, vp, ci, ci, vp, vp, ci, ci, vp, vp, vp, ci, ll] + err
     lib.mix_linear_int_status.argtypes = [C.POINTER(C.c_uint)] + err
+    lib.mix_debug_linear_int_stall.argtypes = [ci]
     lib.mix_expert_combine_grad.argtypes = [vp, ci, ll, ci, vp, vp, ci, ci, ci, vp, ll, vp, vp, ll] + err
     lib.mix_expert_combine.argtypes = [vp, ci, ll, ci, vp, vp, ci, ci, ci, vp, ll] + err
     for name in EXPORTS:

@@ -160,9 +160,10 @@ constexpr int kEpiWarps = 8;                                   // two for each q
 constexpr int kGemmThreads = 64 + 32 * kEpiWarps;              // copies, tensor-core instructions, epilogue
 constexpr int kStageOut = 2048;                                // bytes of a warp's piece of the output on its way to memory
 constexpr long long kI8WaitCycles = 4000000000ll;              // about two seconds
+constexpr long long kI8WaitCyclesTest = 2000000ll;             // ~1 ms: the cap under mix_debug_linear_int_stall
 
 __device__ unsigned g_i8_status;                               // MIX_STATUS_WAIT_TIMEOUT, until mix_linear_int_status reads it
-__device__ const long long g_i8_wait_cycles = kI8WaitCycles;
+std::atomic<int> g_i8_test_stall;                              // host: calls are launched with the test's stall
 
 // kPair: two CTAs of a cluster work on one tile of 256 channels with cta_group::2.  Each holds its own 128 channels and half of the
 // tokens' rows, so that a k-block of 256 tokens costs a CTA 32 KB of copies and 32 KB of reads of shared memory, not 48 and 48:
@@ -192,6 +193,7 @@ struct GemmShared {
   unsigned long long full[12], empty[12], acc_full[2], acc_empty[2];
   unsigned tmem_base;
   int abort_flag;
+  long long wait_cycles;                                       // cap of every bounded wait in this launch
   int row0[kOpMaxExperts + 1];                                 // rows of expert e: row0[e] .. row0[e + 1]
   int tile0[kOpMaxExperts + 1];                                // tiles of expert e
 };
@@ -278,7 +280,7 @@ template <typename OutT, int NT, int kMode>
 __global__ void __launch_bounds__(kGemmThreads, 1)
 linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x, const float* __restrict__ scale,
                   const float* __restrict__ w_scale, const float* __restrict__ bias, const int* __restrict__ offsets, int n_rows, int K,
-                  int N, int E, int tile_tok, int parts, OutT* __restrict__ out, long long ld_out, int vec) {
+                  int N, int E, int tile_tok, int parts, OutT* __restrict__ out, long long ld_out, int vec, int test_stall) {
   using Cfg = GemmCfg<NT, kMode>;
   constexpr bool kPair = Cfg::kPair;
   extern __shared__ unsigned char smem_raw[];
@@ -301,6 +303,7 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
       mbar_init(smem_u32(&sh->acc_empty[a]), kEpiWarps * Cfg::kCtas);
     }
     sh->abort_flag = 0;
+    sh->wait_cycles = test_stall ? kI8WaitCyclesTest : kI8WaitCycles;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -355,7 +358,7 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
   const int tiles = uniform(sh->tile0[E]);
   const LastWave last = !kPair ? LastWave{tiles, 1} : last_wave(tiles, n_workers, tile_tok);
   const int total = kPair ? last.first + (tiles - last.first) * last.pieces : tiles;
-  const long long* cap = &g_i8_wait_cycles;
+  const long long* cap = &sh->wait_cycles;
 
   if (warp == 0) {
     int stage = 0, e = 0;
@@ -374,6 +377,7 @@ linear_int_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
       const unsigned bytes = (Cfg::kABytes + boxes * Cfg::kBoxRows * kKBytes) * Cfg::kCtas;
       for (int kb = kb0; kb < kb1; ++kb) {
         if (!mbar_wait_bounded_warp(smem_u32(&sh->empty[stage]), phase ^ 1u, &sh->abort_flag, cap, &g_i8_status)) { ok = false; break; }
+        if (test_stall) { ok = false; break; }                 // no stage is ever filled: the waits of the others run out
         const unsigned bar = smem_u32(&sh->full[stage]), sa = smem_u32(ring + stage * Cfg::kStageBytes), on = elect_one();
         if (kPair) {
           if (rank == 0) mbar_expect_tx(bar, bytes, on);
@@ -741,7 +745,7 @@ cudaError_t gemm_launch(const Gemm& g, const TilePlan& p, int dev, int n_sms, cu
   cfg.attrs = at;
   cfg.numAttrs = n_at;
   return cudaLaunchKernelEx(&cfg, linear_int_kernel<OutT, NT, kMode>, tw, tx, g.scale, g.w_scale, g.bias, g.offsets, g.n_rows, g.K, g.N, g.E,
-                            p.tile_tok, p.parts, static_cast<OutT*>(g.out), g.ld_out, vec);
+                            p.tile_tok, p.parts, static_cast<OutT*>(g.out), g.ld_out, vec, g_i8_test_stall.load(std::memory_order_relaxed));
 }
 
 // A k-block of a tile of n tokens costs a CTA max(2 n, 256 + n) clocks in a pair and 256 + 2 n alone: the instructions take 2 n, and
@@ -911,6 +915,8 @@ extern "C" int mix_linear_int_grouped(const signed char* codes, const float* sca
   if (!offsets) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "offsets is NULL");
   return gemm_call(Gemm{codes, scale, W, w_scale, bias, offsets, n_rows, K, N, n_experts, out, ld_out}, out_dtype, stream, errbuf, errbuf_len);
 }
+
+extern "C" int mix_debug_linear_int_stall(int on) { return g_i8_test_stall.exchange(on != 0); }
 
 extern "C" int mix_linear_int_status(unsigned* bits, void* stream, char* errbuf, int errbuf_len) {
   if (!bits) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "bits is NULL");
