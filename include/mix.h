@@ -602,7 +602,7 @@ int mix_linear_int_grouped(const signed char* codes, const float* scale, int n_r
                           void* stream, char* errbuf, int errbuf_len);
 
 /* Copy the status word of the 8-bit products on the current device to *bits (host) and clear it: MIX_STATUS_WAIT_TIMEOUT after a bounded wait
-   inside a product kernel ran out, in which case the results since the last call are invalid.  Synchronises `stream`; not capturable. */
+   inside a product kernel ran out, in which case the results since the last call are invalid.  Synchronises `stream`; UNSUPPORTED, and nothing done, while that is captured. */
 int mix_linear_int_status(unsigned* bits, void* stream, char* errbuf, int errbuf_len);
 
 /* Test hook for the time-out path, as MIX_FLAG_TEST_STALL_ENCODE is: products launched while `on` != 0 (of the whole process) never

@@ -921,6 +921,9 @@ extern "C" int mix_debug_linear_int_stall(int on) { return g_i8_test_stall.excha
 extern "C" int mix_linear_int_status(unsigned* bits, void* stream, char* errbuf, int errbuf_len) {
   if (!bits) MIX_OP_FAIL(MIX_ERR_INVALID_ARG, "bits is NULL");
   cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaStreamCaptureStatus capture;
+  MIX_OP_CUDA(cudaStreamIsCapturing(s, &capture));
+  if (capture != cudaStreamCaptureStatusNone) MIX_OP_FAIL(MIX_ERR_UNSUPPORTED, "the status cannot be read in a capture");   // (which goes on)
   const unsigned zero = 0;
   MIX_OP_CUDA(cudaMemcpyFromSymbolAsync(bits, g_i8_status, sizeof(unsigned), 0, cudaMemcpyDeviceToHost, s));
   MIX_OP_CUDA(cudaMemcpyToSymbolAsync(g_i8_status, &zero, sizeof(unsigned), 0, cudaMemcpyHostToDevice, s));

@@ -50,3 +50,17 @@ def test_waits_that_run_out_raise_the_status_and_leave_the_rest_usable(T, K, N, 
         ref = (codes[rows].double() @ w.double().t()) * scale[rows].double()[:, None] * ws.double()[None]
         R.within(out[rows], ref, 3 * R.U * ref.abs() + R.rounding(dtype, ref))
     assert mix.linear_int_status() == 0
+
+
+def test_the_status_call_is_refused_in_a_capture_that_goes_on():
+    codes, scale, W, w_scale = _operands(20, 64, 64)
+    want = mix.linear_int(codes, scale, W, w_scale)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(mix.MixError) as e:
+            mix.linear_int_status()
+        out = mix.linear_int(codes, scale, W, w_scale)
+    assert e.value.code == -3
+    graph.replay()
+    assert torch.equal(out, want) and mix.linear_int_status() == 0
