@@ -924,10 +924,17 @@ extern "C" int mix_linear_int_status(unsigned* bits, void* stream, char* errbuf,
   cudaStreamCaptureStatus capture;
   MIX_OP_CUDA(cudaStreamIsCapturing(s, &capture));
   if (capture != cudaStreamCaptureStatusNone) MIX_OP_FAIL(MIX_ERR_UNSUPPORTED, "the status cannot be read in a capture");   // (which goes on)
+  // Read first, cleared only where something was found: what a product on another stream raises in between is the same bit, which this
+  // call reports.  Copy and clearing one behind the other lost it.
   const unsigned zero = 0;
-  MIX_OP_CUDA(cudaMemcpyFromSymbolAsync(bits, g_i8_status, sizeof(unsigned), 0, cudaMemcpyDeviceToHost, s));
-  MIX_OP_CUDA(cudaMemcpyToSymbolAsync(g_i8_status, &zero, sizeof(unsigned), 0, cudaMemcpyHostToDevice, s));
+  unsigned found = 0;
+  MIX_OP_CUDA(cudaMemcpyFromSymbolAsync(&found, g_i8_status, sizeof(unsigned), 0, cudaMemcpyDeviceToHost, s));
   MIX_OP_CUDA(cudaStreamSynchronize(s));
+  if (found) {
+    MIX_OP_CUDA(cudaMemcpyToSymbolAsync(g_i8_status, &zero, sizeof(unsigned), 0, cudaMemcpyHostToDevice, s));
+    MIX_OP_CUDA(cudaStreamSynchronize(s));
+  }
+  *bits = found;
   return MIX_OK;
 }
 

@@ -64,3 +64,22 @@ def test_the_status_call_is_refused_in_a_capture_that_goes_on():
     assert e.value.code == -3
     graph.replay()
     assert torch.equal(out, want) and mix.linear_int_status() == 0
+
+
+def test_a_wait_that_runs_out_while_the_status_is_read_is_not_lost():
+    """A product of one CTA runs into its time-out on one stream while another reads the word over and over."""
+    codes, scale, W, w_scale = _operands(20, 64, 64)
+    lib = mix.load_library()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    assert mix.linear_int_status() == 0
+    for trial in range(400):
+        lib.mix_debug_linear_int_stall(1)
+        try:
+            mix.linear_int(codes, scale, W, w_scale, stream=side)
+        finally:
+            lib.mix_debug_linear_int_stall(0)
+        seen = 0
+        while not side.query():
+            seen |= mix.linear_int_status()
+        assert seen | mix.linear_int_status() == WAIT_TIMEOUT, trial
