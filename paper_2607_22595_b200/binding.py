@@ -79,12 +79,11 @@ class MixError(RuntimeError):
 
 _lib = None
 _fast = None          # the CPython module of the calls a step makes (csrc/fastcall.c), loaded with the library
-_ops = None           # the one of the calls without a context (csrc/fastops.cpp; experts.py)
 
 
 def load_library(path: Optional[str] = None) -> C.CDLL:
     """Load libmix.so (built in-tree).  Raises if it is absent: there is no other path."""
-    global _lib, _fast, _ops
+    global _lib, _fast
     if _lib is not None and path is None:
         return _lib
     path = path or _build.LIB_PATH
@@ -138,8 +137,8 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
         if name != "mix_last_error":
             getattr(lib, name).restype = ll if name.endswith("_workspace") and name != "mix_debug_workspace" else ci
     if path == _build.LIB_PATH:
-        from . import _fastcall, _fastops
-        _lib, _fast, _ops = lib, _fastcall, _fastops
+        from . import _fastcall
+        _lib, _fast = lib, _fastcall
     return lib
 
 

@@ -15,6 +15,7 @@
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/version.h>
 
 #include <climits>
 #include <cstdarg>
@@ -493,4 +494,9 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastops", nullptr, -1, methods, n
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__fastops(void) { return PyModule_Create(&module); }
+// The layout of torch's C++ objects is compiled in: experts.py compares this with the torch that is running.
+PyMODINIT_FUNC PyInit__fastops(void) {
+  PyObject* m = PyModule_Create(&module);
+  if (m && PyModule_AddStringConstant(m, "torch_version", TORCH_VERSION) != 0) Py_CLEAR(m);
+  return m;
+}
