@@ -402,13 +402,22 @@ struct Plan {
 // 8192 rows of 64 bf16: 9.8 us, 11.3 with 64 rows).  Where requests are short (decode steps: one row each) a unit is one warp and no
 // barrier stands between two requests; each costs it a microsecond and a half, so a unit has 4 rows as long as the SMs hold all
 // units at once (1024 requests of one row, 64 experts: 10.6 us, 46 with 32 rows).
+// A lane adds the probabilities of an expert up in fp32, so it takes no more than 64 rows: beyond 303104 rows of more than 128 experts the
+// units make several waves.  (A small call is within it: 16384 logits are 64 rows a lane at most.)
 constexpr int kDirectLogits = 16384;
+constexpr int kLaneRows = 64;
+int rows_of_a_warp(int E) {                                     // held at a time: 32 / G of MIX_ROW_LAYOUT
+  int rows = 32;
+  while (rows > 1 && 256 / rows < E) rows /= 2;
+  return rows;
+}
 Plan plan(int T, int E, int n_seg, int n_sms) {
   Plan p;
   p.direct = (long long)T * E <= kDirectLogits;
   p.warps = T / n_seg >= 64 ? kUnitWarps : 1;
   if (p.warps == kUnitWarps) {
-    p.unit_rows = (T + kUnitCtas * n_sms - 1) / (kUnitCtas * n_sms);
+    const int wave = kUnitCtas * n_sms, most = kUnitWarps * rows_of_a_warp(E) * kLaneRows, waves = (T - 1) / (wave * most) + 1;
+    p.unit_rows = (T - 1) / (wave * waves) + 1;
     if (p.unit_rows < 32) p.unit_rows = 32;
   } else {
     p.unit_rows = T <= 8 * 32 * n_sms ? 4 : 32;

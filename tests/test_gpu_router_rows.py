@@ -100,3 +100,18 @@ def test_balance_of_logits_far_from_0(E, k, dtype, act):
     T = x.shape[0]
     check_balance(x, k, act, None)
     check_balance(x, k, act, [0, 1, 2, 7, 50, 51, T // 2, T - 3, T])
+
+
+@pytest.mark.parametrize("T,E,act", [(6_000_000, 300, "softmax"), (6_000_000, 130, "sigmoid"), (12_000_000, 64, "softmax")])
+def test_mean_probabilities_of_millions_of_rows(T, E, act):
+    """Rows that are all alike: every addition of a probability rounds to the same side, and the error is that of the longest run of
+    additions in fp32.  Runs of at most 64, and 8 to put them together, as in short batches."""
+    row = torch.randn(E, generator=torch.Generator().manual_seed(E)).to(torch.bfloat16)
+    x = row.to(DEV).repeat(T, 1)
+    idx = torch.zeros((T, 1), dtype=torch.int32, device=DEV)
+    loss, counts, mean_p, rows = mix.router_balance(x, idx, act=ACT[act])
+    p = R.probabilities(row.double()[None], act)
+    bound = row_bound(row[None], act) + 72 * R.U
+    assert rows.item() == T and counts[0, 0].item() == T
+    R.within(mean_p.cpu(), p, bound * p)
+    R.within(loss.cpu(), E * p[:, 0], bound[0] * E * p[:, 0])
