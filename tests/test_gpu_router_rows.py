@@ -115,3 +115,42 @@ def test_mean_probabilities_of_millions_of_rows(T, E, act):
     assert rows.item() == T and counts[0, 0].item() == T
     R.within(mean_p.cpu(), p, bound * p)
     R.within(loss.cpu(), E * p[:, 0], bound[0] * E * p[:, 0])
+
+
+def ordinary_logits(T, E, dtype, seed, special=True):
+    """Logits within some ten of each other, a few rows with experts forced in or out."""
+    g = torch.Generator().manual_seed(seed)
+    x = 2 * torch.randn((T, E), generator=g)
+    if special and T >= 8:
+        x[1] = -torch.inf
+        x[2, E // 2:] = -torch.inf
+        x[3, E // 3] = torch.inf
+        x[5, 0] = torch.nan
+        x[6] = torch.round(x[6])
+    return x.to(DTYPES[dtype]).to(DEV)
+
+
+@pytest.mark.parametrize("T,E,k", [(1, 8, 2), (64, 8, 2), (33, 9, 2), (40, 16, 16), (29, 31, 4), (70, 33, 6), (64, 64, 8), (31, 100, 16), (19, 160, 6), (50, 256, 8),
+                                   (20, 257, 8), (24, 512, 16), (300, 64, 6)])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("act,renorm", [("softmax", True), ("softmax", False), ("sigmoid", True), ("sigmoid", False)])
+def test_selection_with_a_bound_for_each_row(T, E, k, dtype, act, renorm):
+    check_topk(ordinary_logits(T, E, dtype, T + E), k, act, renorm)
+
+
+# more than 37888 rows in requests of fewer than 64: units of one warp and 32 rows; 62 rows in one segment and more than 16384 logits: units of
+# one warp, their sums put together by a cluster; the others as they come
+BALANCES = [(40000, 24, 3, "many"), (62, 300, 5, "one"), (63, 512, 8, "one"), (50000, 100, 6, "many"), (3000, 64, 6, "many"), (40, 8, 2, "one"),
+            (517, 8, 2, "two"), (2500, 160, 8, "two"), (20000, 33, 4, "two")]
+
+
+@pytest.mark.parametrize("T,E,k,kind", BALANCES)
+@pytest.mark.parametrize("dtype,act", [("fp32", "softmax"), ("bf16", "softmax"), ("fp16", "sigmoid"), ("fp32", "sigmoid")])
+def test_balance_with_a_bound_for_each_segment(T, E, k, kind, dtype, act):
+    seg = None
+    if kind == "two":
+        seg = [0, T // 3, T - 5]
+    elif kind == "many":                                       # ragged, some empty, the first and the last rows in none
+        cuts = torch.randint(3, T - 9, (2000,), generator=torch.Generator().manual_seed(T)).tolist()
+        seg = sorted(cuts + cuts[:200])
+    check_balance(ordinary_logits(T, E, dtype, T + E), k, act, seg)
