@@ -434,6 +434,9 @@ PyObject* expert_combine(PyObject* const* a) {
 
 // expert_combine_grad(d_out, y, weights, position, want_y, d_weights | None, d_y | None, stream | None)
 PyObject* expert_combine_grad(PyObject* const* a) {
+  const int want_y = PyObject_IsTrue(a[4]);
+  if (want_y < 0) throw Raised();
+  need(want_y || a[6] == Py_None, "d_y is given, but want_y is not set");
   const Rows y = rows_of(tensor(a[1], "y", 2), "y");
   const Tensor& pt = tensor(a[3], "position", ScalarType::Int, 2, &y.t);
   const int64_t T = pt.size(0), k = pt.size(1);
@@ -441,8 +444,6 @@ PyObject* expert_combine_grad(PyObject* const* a) {
   const float* w = dense<float>(a[2], "weights", ScalarType::Float, {T, k}, y.t);
   const Rows d = rows_of(tensor(a[0], "d_out", 2, &y.t), "d_out");
   need(d.n == T && d.m == y.m && d.dtype == y.dtype, "d_out must be [T, N] in y's type");
-  const int want_y = PyObject_IsTrue(a[4]);
-  if (want_y < 0) throw Raised();
   Call c(y.t.get_device(), a[7]);
   Results r;
   float* dw;
