@@ -16,12 +16,16 @@ def row_bound(x, act):
     from the row's largest (at most 104), or of e^x where the scores are sigmoids: a power of 2 whose argument is off by 1.22 |d| U (its
     rounding, and log2 e's) and two steps, 4 U.  The difference is exact where the logits are that close to each other and far from
     0.  The sum of the row's terms is off by the mean of that, at most 17 U, and 24 U of additions; reciprocal and products 4 U."""
-    x = torch.where(torch.isfinite(x), x.double(), 0.0)
-    d = x.amax(1, keepdim=True) - x
+    x = x.double()
+    there = torch.isfinite(x)
+    far = _that_count(torch.where(there, torch.where(there, x, -torch.inf).amax(1, keepdim=True) - x, 0.0))
     if act == "sigmoid":
-        d = torch.maximum(d, x.abs())
-    far = torch.where(d < 104, d, 0.0).amax(1, keepdim=True)
+        far = torch.maximum(far, _that_count(torch.where(there, x.abs(), 0.0)))     # each by itself: -40 counts beside 200, though they are 240 apart
     return (2 * (far + 8) + 32) * R.U
+
+
+def _that_count(d):
+    return torch.where(d < 104, d, 0.0).amax(1, keepdim=True)
 
 
 def check_topk(x, k, act, renorm):
