@@ -611,7 +611,7 @@ int mix_linear_int_status(unsigned* bits, void* stream, char* errbuf, int errbuf
 int mix_debug_linear_int_stall(int on);
 
 /* The experts' results summed over each token's experts: out[t, :] = sum_j weights[t, j] y[position[t, j], :], j rising, in fp32, rounded
-   once.  y: dtype [y_rows, N], rows ld_y apart, in mix_expert_order()'s order; position int32 [T, k] from the same call, entries outside
+   once (results that were left in 16 bits have been rounded before; fp32 ones keep the sum's precision).  y: dtype [y_rows, N], rows ld_y apart, in mix_expert_order()'s order; position int32 [T, k] from the same call, entries outside
    [0, y_rows) do not count (nor what stands in their weights).  out: dtype [T, N], rows ld_out apart; a token without experts gets zeros.
    out may not overlap y.
    Errors: OUT_OF_RANGE (T < 0, N outside [1, MIX_COMBINE_MAX_N], k outside [1, 16], ld below N), INVALID_ARG. */

@@ -140,8 +140,9 @@ __device__ __forceinline__ bool group_any(bool yes) {
 }
 
 // e^x as 2^(x log2 e) by the hardware's 2^x: the argument is off by half a step of itself (|x| U, U = 2^-24) and by what log2 e is off
-// (0.22 |x| U), the result by two steps (4 U).  expf takes seven instructions to save the first; a logit's distance from the row's
-// largest is rounded by as much already.  Results below 2^-126 are 0.
+// (0.22 |x| U), the result by two steps (4 U).  A logit's distance from the row's largest is rounded by as much already.  Results below
+// 2^-126 are 0.  (65536 rows of 256 fp32, k = 8, with expf(x - top) instead: selection with the whole row's softmax 34.0 us, 32.5 so, its gradient
+// 24.4, 23.2 so; balance loss of sigmoids 26.1 forward, 27.9 so, and 30.0 backward, 29.8 so.)
 __device__ __forceinline__ float exp2_hw(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

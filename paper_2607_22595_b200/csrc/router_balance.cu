@@ -11,8 +11,8 @@
 // cluster of CTAs per segment where a segment has many.  Both add in a fixed order.
 // Backward: one pass over the logits, a warp per run of rows.
 //
-// 65536 rows of 256 fp32 in 16 segments, sigmoid: forward 23.5 us (16 + 7 in its two launches; the logits' stream takes 10.3),
-// backward 29.3 (20.6 read and written).  What bounds both is issue: 14 instructions a logit, two of them on the special-function
+// 65536 rows of 256 fp32 in 16 segments, k = 8, sigmoid: forward 28.0 us (21 and 7 in its two launches; the logits' stream takes 10.3),
+// backward 29.8 (20.6 read and written).  What bounds both is issue: 14 instructions a logit, two of them on the special-function
 // unit, beside the reductions of a row.
 #include "op_common.cuh"
 #include "tc_common.cuh"
@@ -22,8 +22,9 @@ using namespace mix;
 namespace {
 
 constexpr int kUnitWarps = 8;              // warps of a unit where requests are long
-// CTAs an SM holds at a time: large batches make one wave of them.  Above 256 experts, with 16 logits a lane, that spills 140 bytes and is
-// faster all the same: 32768 rows of 512 fp32, forward 23.7 us and backward 31.3, 27.1 and 32.7 with three and two CTAs.
+// CTAs an SM holds at a time: large batches make whole waves of them.  Above 256 experts, with 16 logits a lane, the backward spills 140 bytes
+// for it (the forward of small calls 32, the forward in units nothing) and is faster all the same: 32768 rows of 512 fp32, forward 23.9
+// us and backward 31.3, 27.1 and 32.7 with three and two CTAs.
 constexpr int kUnitCtas = 4, kGradCtas = 4;
 constexpr int kFinThreads = 512;
 constexpr int kFinCluster = 8;

@@ -49,7 +49,8 @@ def router_topk(logits, k, act=MIX_ACT_SOFTMAX, renormalise=True, n_live=None, i
     """The k largest logits of each row -> idx int32 [T, k] (largest first, of equal ones the lower index first) and weights
     fp32 [T, k]: their softmax or sigmoid values, divided by their sum where `renormalise`.  logits: fp32, bf16 or fp16
     [T, n_experts].  -inf and NaN are never chosen (-1, weight 0, where fewer than k are left), +inf shares the row.  n_live: int32[1]
-    on the device; rows from there on are padding and get -1 and 0."""
+    on the device; rows from there on are padding and get -1 and 0.  New outputs are parts of one allocation: who keeps or saves the one
+    keeps or saves both (clone it, or give buffers)."""
     return (_loaded or _ops()).router_topk(logits, k, act, renormalise, n_live, idx, weights, stream)
 
 
@@ -60,14 +61,16 @@ def router_topk_grad(logits, idx, weights, d_weights, act=MIX_ACT_SOFTMAX, renor
 
 def expert_order(idx, n_experts, offsets=None, order=None, position=None, stream=None):
     """The entries of idx int32 [T, k] sorted by expert, stably -> offsets int32 [n_experts + 1], order int32 [T * k] (entries
-    t * k + j, -1 behind the last), position int32 [T, k] (the entry's place in `order`, -1 where it names no expert)."""
+    t * k + j, -1 behind the last), position int32 [T, k] (the entry's place in `order`, -1 where it names no expert).  New outputs are
+    parts of one allocation."""
     return (_loaded or _ops()).expert_order(idx, n_experts, offsets, order, position, stream)
 
 
 def router_balance(logits, idx, seg=None, act=MIX_ACT_SOFTMAX, stream=None):
     """Per segment of rows (seg int32 [n + 1], offsets on the device; None: all rows are one segment): the balance loss fp32 [n], how
     often each expert was chosen int32 [n, n_experts], the experts' mean probabilities fp32 [n, n_experts] and the rows counted
-    int32 [n].  idx int32 [T, k] as from router_topk; rows that name no expert do not count."""
+    int32 [n].  idx int32 [T, k] as from router_topk; rows that name no expert do not count.  The four are parts of one allocation: who keeps
+    the loss keeps counts and mean probabilities too (clone it)."""
     return (_loaded or _ops()).router_balance(logits, idx, seg, act, stream)
 
 
@@ -78,7 +81,7 @@ def router_balance_grad(logits, idx, counts, rows, d_loss, seg=None, act=MIX_ACT
 
 def quantize_rows(x, order=None, k=1, codes=None, scale=None, stream=None):
     """Rows of x (bf16 or fp16 [T, d], d a multiple of 16) as 8-bit integers: codes int8 [n, d] and scale fp32 [n], codes * scale being
-    the nearest to x.  With `order` (expert_order's, int32 [n]) row i is row order[i] // k of x; entries of -1 give zeros."""
+    the nearest to x.  With `order` (expert_order's, int32 [n]) row i is row order[i] // k of x; entries of -1 give zeros.  New outputs are parts of one allocation."""
     return (_loaded or _ops()).quantize_rows(x, order, k, codes, scale, stream)
 
 
@@ -106,7 +109,8 @@ def linear_int_status(stream=None) -> int:
 
 
 def expert_combine(y, weights, position, out=None, stream=None):
-    """out[t] = sum_j weights[t, j] y[position[t, j]] -> [T, N] in y's type.  y [n, N] in expert_order's order; entries of -1 do not count."""
+    """out[t] = sum_j weights[t, j] y[position[t, j]] -> [T, N] in y's type.  y [n, N] in expert_order's order; entries of -1 do not count.
+    The sum is taken in fp32; results in 16 bits have been rounded before it, fp32 ones (linear_int_grouped's dtype) have not."""
     return (_loaded or _ops()).expert_combine(y, weights, position, out, stream)
 
 
